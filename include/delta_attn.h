@@ -26,10 +26,10 @@
  *             delta_delta_attn_select for the same shape and selection parameters.
  *   Layouts.  bf16 = IEEE bfloat16 bits.  q, out: [batch, n_q_heads, head_dim].
  *             k_cache, v_cache: [n_phys_pages, n_kv_heads, page_size, head_dim] (one contiguous
- *             page_size x head_dim tile per page and KV head).
+ *             page_size x head_dim tile per page and KV head), bf16 or e4m3 (delta_kv_t.kv_type).
  *             page_table: int32 [batch, max_pages_per_seq], logical page -> physical page.
  *             Query head j reads KV head j / (n_q_heads / n_kv_heads).
- *   Numerics. bf16 inputs, fp32 accumulation and online softmax, bf16 round-to-nearest-even
+ *   Numerics. bf16 queries, fp32 accumulation and online softmax, bf16 round-to-nearest-even
  *             outputs.  Results are deterministic: the same inputs and shape give bitwise
  *             identical outputs, and a DELTA layer's attention output is bitwise identical to
  *             delta_full_attn's on the same inputs when it runs the split path (with the fused
@@ -85,14 +85,25 @@ typedef struct {
   float sm_scale;             /* softmax scale; 0 selects 1/sqrt(head_dim) (Eq. gqa_attention) */
 } delta_shape_t;
 
-/* One layer's paged KV cache (Sec. 4 "Page-based DELTA"; never evicted, Sec. 4). */
+/* What a KV cache holds: bf16, or the 8-bit float e4m3 (OCP FP8: 4 exponent and 3 mantissa bits,
+ * largest finite value 448, no infinity).  An e4m3 value stands for itself times the scale of its
+ * KV head: key = k * k_scale[h], value = v * v_scale[h].  Half the bytes of every layer, at a
+ * relative rounding of at most 2^-4 per value. */
+enum { DELTA_KV_BF16 = 0, DELTA_KV_E4M3 = 1 };
+
+/* One layer's paged KV cache (Sec. 4 "Page-based DELTA"; never evicted, Sec. 4).  The layers of a
+ * step may differ in kv_type. */
 typedef struct {
-  const void* k_cache;        /* bf16 [n_phys_pages, n_kv_heads, page_size, head_dim]         */
-  const void* v_cache;        /* bf16, same layout                                            */
+  const void* k_cache;        /* [n_phys_pages, n_kv_heads, page_size, head_dim] of kv_type   */
+  const void* v_cache;        /* same type and layout                                         */
   const int32_t* page_table;  /* int32 [batch, max_pages_per_seq]                             */
   const int32_t* seq_lens;    /* int32 [batch]: tokens cached, the current one included       */
   int64_t n_pages;            /* n_phys_pages, or 0 if not stated; read by the debug build's
                                  checks of page-table entries only                           */
+  int32_t kv_type;            /* DELTA_KV_BF16 (0) or DELTA_KV_E4M3: element type of both
+                                 caches (sizes and layouts above count elements)             */
+  const float* k_scale;       /* fp32 [n_kv_heads], positive and finite; NULL: all 1.  e4m3   */
+  const float* v_scale;       /* caches only (NULL with bf16)                                */
 } delta_kv_t;
 
 /* Selection parameters (Sec. 4; App. A, Alg. 2).  All counts are in TOKENS.  The budget must
@@ -114,8 +125,8 @@ typedef struct {
  *   DELTA_PATH_SPLIT  attention (logits staged through the workspace), scoring and selection
  *                     launches; the layer's attention output is bitwise delta_full_attn's.
  *   DELTA_PATH_FUSED  one kernel that keeps the logits on chip, wherever it can run: head_dim
- *                     128, a multiple of 4 KV heads, at most 32 query heads, at most 2048
- *                     candidate units and a grid of ceil(max_seq_len / 1024) x batch workgroups
+ *                     128, a bf16 cache, a multiple of 4 KV heads, at most 32 query heads, at
+ *                     most 2048 candidate units and a grid of ceil(max_seq_len / 1024) x batch workgroups
  *                     that the device holds at once; elsewhere the split launches.  Its output
  *                     equals delta_full_attn's up to floating-point summation order (within the
  *                     bf16 rounding of the result), not bit for bit.
@@ -168,7 +179,8 @@ int delta_delta_attn_select(const delta_shape_t* shape, const delta_kv_t* kv, co
                             size_t ws_bytes, void* stream);
 
 /* Which path delta_delta_attn_select takes for this shape and selection (sel->delta_path) on
- * the current device: *fused = 1 for the fused kernel, 0 for the attention, scoring and
+ * the current device with a bf16 cache (an e4m3 cache always takes the split path, whatever
+ * sel->delta_path): *fused = 1 for the fused kernel, 0 for the attention, scoring and
  * selection launches.  Host only; it queries the current device's CU count and its occupancy
  * for the fused kernel (without a device: 0 unless the kernel cannot apply anyway).  Errors as
  * delta_workspace_bytes; `sel` and `fused` must be non-NULL. */

@@ -68,11 +68,12 @@ constexpr int kPageMask = 0x3fffffff;
 constexpr int kPartialPage = 0x40000000;
 constexpr int kEmptyPage = (int)0x80000000;
 
-template <int D, int G, int MODE, bool LOGITS, bool BAL>
+template <int D, int G, int MODE, bool LOGITS, bool BAL, bool KV8>
 __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(const AttnArgs a) {
   static_assert(!BAL || MODE == ROWS_DENSE, "the balanced decomposition is for dense launches");
   using Gm = Geo<D>;
-  constexpr int R = Gm::R;
+  using CacheTile = std::conditional_t<KV8, Tile8<D>, Tile<D>>;
+  constexpr int R = KV8 ? Geo8<D>::R : Gm::R;
   constexpr int T = kAttnThreads, NW = T / 64;
   constexpr int kSeg = kMaxRowSlots / (MODE == ROWS_SEL_TOKEN ? 16 : 1);   // groups listed at once
   static_assert(kSeg % (4 * NW) == 0, "a wave's share of a piece does not depend on the listing");
@@ -173,38 +174,60 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
     // but reads nothing (a page tile) or one cache line per load instruction (gathered rows).
     const int s_last_page = (s_b - 1) >> 4;
     const uint32_t tail_mask = 0xffffu >> (15 - ((s_b - 1) & 15));   // rows of the last page
-    auto load_tile = [&](Tile<D>& t, int row, int li, int l0, bool real) {
-      if (MODE == ROWS_SEL_TOKEN) {
+    auto load_tile = [&](CacheTile& t, int row, int li, int l0, bool real) {
+      const uint8_t* k8 = reinterpret_cast<const uint8_t*>(a.k_cache);
+      const uint8_t* v8 = reinterpret_cast<const uint8_t*>(a.v_cache);
+      if constexpr (MODE == ROWS_SEL_TOKEN) {
         // every row is its own (page, row); rows past the selection re-read the group's first
         const int* rows = s_rows + 16 * li;
         const int first = rows[0];
         t.kmask = (uint32_t)__ballot(rows[hcol] >= 0 && 16 * (l0 + li) + hcol < sel_n) & 0xffffu;
-#pragma unroll
-        for (int i = 0; i < Gm::NK; ++i) {
-          const int r = k_row<D>(i, lane);
+        // element offset of row r of the group
+        auto at = [&](int r) {
           const int kr = ((t.kmask >> r) & 1u) && real ? rows[r] : first;
-          t.k[i] = load16_stream(a.k_cache + (size_t)(kr >> 4) * a.page_stride + head_off +
-                                 (size_t)(kr & 15) * D + (real ? 8 * (lane % Gm::CPR) : 0));
-        }
+          return (size_t)(kr >> 4) * a.page_stride + head_off + (size_t)(kr & 15) * D;
+        };
+        if constexpr (KV8) {
+          using G8 = Geo8<D>;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 4 * quad + i;
-          const int vr = ((t.kmask >> r) & 1u) && real ? rows[r] : first;
-          t.v[i] = load_v_stream<D>(a.v_cache + (size_t)(vr >> 4) * a.page_stride + head_off +
-                                    (size_t)(vr & 15) * D + (real ? Gm::NC * hcol : 0));
+          for (int i = 0; i < G8::NL; ++i)
+            t.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
+                k8 + at(G8::RPL * i + lane / G8::CPR) + (real ? 16 * (lane % G8::CPR) : 0)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint8_t* vp = v8 + at(4 * quad + i) + (real ? Gm::NC * hcol : 0);
+            if constexpr (D == 128) {
+              const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vp));
+              t.v[i][0] = w[0];
+              t.v[i][1] = w[1];
+            } else {
+              t.v[i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(vp));
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < Gm::NK; ++i)
+            t.k[i] = load16_stream(a.k_cache + at(k_row<D>(i, lane)) + (real ? 8 * (lane % Gm::CPR) : 0));
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            t.v[i] = load_v_stream<D>(a.v_cache + at(4 * quad + i) + (real ? Gm::NC * hcol : 0));
         }
       } else {
         row = __builtin_amdgcn_readfirstlane(row);
         const size_t page = (size_t)(row & kPageMask) * a.page_stride + head_off;
         if (MODE == ROWS_DENSE) t.kmask = l0 + li == s_last_page ? tail_mask : 0xffffu;
         else t.kmask = row < 0 ? 0u : (row & kPartialPage) ? tail_mask : 0xffffu;
-        load_page_tile<D>(t, a.k_cache + page, a.v_cache + page, real, lane);
+        if constexpr (KV8) load_page_tile<D>(t, k8 + page, v8 + page, real, lane);
+        else load_page_tile<D>(t, a.k_cache + page, a.v_cache + page, real, lane);
       }
     };
 
     WaveSoftmax<D, G> st;
     st.init();
     const int Hq_row = b * Hq + g * G;
+    // an e4m3 cache's scales: the K scale joins the scores', the V scale the outputs'
+    const float scale = KV8 && a.k_scale ? a.scale_log2 * a.k_scale[g] : a.scale_log2;
+    const float v_scale = KV8 && a.v_scale ? a.v_scale[g] : 1.f;
     // Logits on: the workgroup keeps the logits of a chunk of kChunk groups in LDS ([group]
     // [head][16], the global layout) and writes the chunk out cooperatively between chunks.
     // Bound: the writes, which HBM takes at about 2.5 TB/s while it serves the other workgroups'
@@ -213,19 +236,21 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
     // written through (sc1) against non-temporal and ordinary ones, us per Delta layer: 222.5,
     // 228.5, 231; 16 x 32K with 32/8 heads 373, 378, 387; 32 ragged 16K-32K 616, 623, 644.
 #if DELTA_QK_VALU
-    // build option: QK^T on the vector ALUs, the query vectors read from the wave's LDS copy
+    // build option: QK^T on the vector ALUs (bf16 caches), the query vectors read from the wave's
+    // LDS copy
     stage_query_lds<D, G>(qb, s_qv[wave], lane);
     wave_lds_sync();
-    auto process = [&](Tile<D>& t, int slot_in_chunk) {
-      process_tile_valu<D, G, LOGITS>(t, s_qv[wave], a.scale_log2, st, s_p[wave], s_w[wave].k,
-                                      s_stage + slot_in_chunk * G * 16, lane);
-    };
-#else
-    auto process = [&](Tile<D>& t, int slot_in_chunk) {
-      process_tile<D, G, LOGITS>(t, qb, a.scale_log2, st, s_w[wave].k,
-                                 s_stage + slot_in_chunk * G * 16, lane);
-    };
 #endif
+    auto process = [&](CacheTile& t, int slot_in_chunk) {
+      float* logit_slot = s_stage + slot_in_chunk * G * 16;
+#if DELTA_QK_VALU
+      if constexpr (!KV8) {
+        process_tile_valu<D, G, LOGITS>(t, s_qv[wave], scale, st, s_p[wave], s_w[wave].k, logit_slot, lane);
+        return;
+      }
+#endif
+      process_tile<D, G, LOGITS>(t, qb, scale, st, s_w[wave].k, logit_slot, lane);
+    };
 
     // The waves take a piece's groups in turn: one at a time in short pieces, so that every wave
     // has its share, and blocks of four in pieces of 128 groups or more, where pages in order
@@ -250,13 +275,13 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
       // (the scheduler must not reorder the loads of different tiles: the compiler's wait for
       // the oldest tile would then drain the younger ones)
       int row = s_rows[MODE == ROWS_SEL_TOKEN ? 0 : group_of(kb)];
-      auto fetch = [&](Tile<D>& t, int k) {
+      auto fetch = [&](CacheTile& t, int k) {
         __builtin_amdgcn_sched_barrier(0);
         load_tile(t, row, group_of(min(k, ke - 1)), l0, k < ke);
         if (MODE != ROWS_SEL_TOKEN) row = s_rows[group_of(min(k + 1, ke - 1))];
         __builtin_amdgcn_sched_barrier(0);
       };
-      Tile<D> t[R];
+      CacheTile t[R];
 #pragma unroll
       for (int i = 0; i < R - 1; ++i) fetch(t[i], kb + i);
       for (int k = kb; k < ke; k += R) {
@@ -328,7 +353,8 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
         L += f * s_l[w][h];
       }
     }
-    auto store_out = [&](const f32x4& v, float lsum, float mx) {
+    auto store_out = [&](f32x4 v, float lsum, float mx) {
+      if (KV8) v *= v_scale;
       // (divided, not multiplied by 1 / lsum: that product's extra rounding moves quotients half
       // way between two bf16 values, as equal weights give)
       uint2 packed;
@@ -595,46 +621,50 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
   }
 }
 
-template <int D, int G>
+template <int D, int G, bool KV8>
 hipError_t launch_dg(int mode, const AttnArgs& a, int batch, hipStream_t stream) {
   const dim3 grid(a.n_split, a.n_kv_heads, batch), block(kAttnThreads);
   switch (mode) {
     case ROWS_DENSE:
       // the balanced decomposition is a separate instantiation, so that launches which cannot
       // take it run the static kernel's code (0.5-1 us of a launch of 8-12)
-      if (a.logits && a.n_runs > 0) hipLaunchKernelGGL((attn_kernel<D, G, ROWS_DENSE, true, true>), grid, block, 0, stream, a);
-      else if (a.logits) hipLaunchKernelGGL((attn_kernel<D, G, ROWS_DENSE, true, false>), grid, block, 0, stream, a);
-      else if (a.n_runs > 0) hipLaunchKernelGGL((attn_kernel<D, G, ROWS_DENSE, false, true>), grid, block, 0, stream, a);
-      else hipLaunchKernelGGL((attn_kernel<D, G, ROWS_DENSE, false, false>), grid, block, 0, stream, a);
+      if (a.logits && a.n_runs > 0) hipLaunchKernelGGL((attn_kernel<D, G, ROWS_DENSE, true, true, KV8>), grid, block, 0, stream, a);
+      else if (a.logits) hipLaunchKernelGGL((attn_kernel<D, G, ROWS_DENSE, true, false, KV8>), grid, block, 0, stream, a);
+      else if (a.n_runs > 0) hipLaunchKernelGGL((attn_kernel<D, G, ROWS_DENSE, false, true, KV8>), grid, block, 0, stream, a);
+      else hipLaunchKernelGGL((attn_kernel<D, G, ROWS_DENSE, false, false, KV8>), grid, block, 0, stream, a);
       break;
-    case ROWS_SEL_PAGE: hipLaunchKernelGGL((attn_kernel<D, G, ROWS_SEL_PAGE, false, false>), grid, block, 0, stream, a); break;
-    case ROWS_SEL_TOKEN: hipLaunchKernelGGL((attn_kernel<D, G, ROWS_SEL_TOKEN, false, false>), grid, block, 0, stream, a); break;
+    case ROWS_SEL_PAGE: hipLaunchKernelGGL((attn_kernel<D, G, ROWS_SEL_PAGE, false, false, KV8>), grid, block, 0, stream, a); break;
+    case ROWS_SEL_TOKEN: hipLaunchKernelGGL((attn_kernel<D, G, ROWS_SEL_TOKEN, false, false, KV8>), grid, block, 0, stream, a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
 }
 
-template <int D>
+template <int D, bool KV8>
 hipError_t launch_d(int group, int mode, const AttnArgs& a, int batch, hipStream_t stream) {
   switch (group) {
-    case 1: return launch_dg<D, 1>(mode, a, batch, stream);
-    case 2: return launch_dg<D, 2>(mode, a, batch, stream);
-    case 3: return launch_dg<D, 3>(mode, a, batch, stream);
-    case 4: return launch_dg<D, 4>(mode, a, batch, stream);
-    case 5: return launch_dg<D, 5>(mode, a, batch, stream);
-    case 6: return launch_dg<D, 6>(mode, a, batch, stream);
-    case 7: return launch_dg<D, 7>(mode, a, batch, stream);
-    case 8: return launch_dg<D, 8>(mode, a, batch, stream);
+    case 1: return launch_dg<D, 1, KV8>(mode, a, batch, stream);
+    case 2: return launch_dg<D, 2, KV8>(mode, a, batch, stream);
+    case 3: return launch_dg<D, 3, KV8>(mode, a, batch, stream);
+    case 4: return launch_dg<D, 4, KV8>(mode, a, batch, stream);
+    case 5: return launch_dg<D, 5, KV8>(mode, a, batch, stream);
+    case 6: return launch_dg<D, 6, KV8>(mode, a, batch, stream);
+    case 7: return launch_dg<D, 7, KV8>(mode, a, batch, stream);
+    case 8: return launch_dg<D, 8, KV8>(mode, a, batch, stream);
     default: return hipErrorInvalidValue;
   }
 }
 
 }  // namespace
 
-hipError_t launch_attention(int head_dim, int group, int mode, const AttnArgs& a, int batch,
+hipError_t launch_attention(int head_dim, int group, int mode, bool kv8, const AttnArgs& a, int batch,
                             hipStream_t stream) {
-  if (head_dim == 128) return launch_d<128>(group, mode, a, batch, stream);
-  if (head_dim == 64) return launch_d<64>(group, mode, a, batch, stream);
+  if (head_dim == 128)
+    return kv8 ? launch_d<128, true>(group, mode, a, batch, stream)
+               : launch_d<128, false>(group, mode, a, batch, stream);
+  if (head_dim == 64)
+    return kv8 ? launch_d<64, true>(group, mode, a, batch, stream)
+               : launch_d<64, false>(group, mode, a, batch, stream);
   return hipErrorInvalidValue;
 }
 

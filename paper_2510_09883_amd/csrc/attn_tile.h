@@ -85,6 +85,31 @@ struct Tile {
   uint32_t kmask;   // bit r: row r valid (wave-uniform)
 };
 
+// The same tile of an e4m3 cache as it comes from memory: half the words, expanded to bf16 (exactly:
+// an e4m3 value has 4 significant bits and exponents that bf16 has too) when the tile is consumed,
+// K on its way into the LDS slice, V in registers.  The expansion costs one instruction per two
+// values; what a wave keeps in flight are the 8-bit words, so R may be larger.
+template <int D>
+struct Geo8 {
+  static constexpr int NL = D / 64;      // 16-byte K loads per lane per tile
+  static constexpr int CPR = D / 16;     // 16-byte pieces of a K row
+  static constexpr int RPL = 64 / CPR;   // K rows per wave-wide load
+  static constexpr int R = D == 128 ? 5 : 6;
+};
+
+template <int D>
+struct Tile8 {
+  u32x4 k[Geo8<D>::NL];   // load i: row RPL * i + lane / CPR, piece lane % CPR
+  uint32_t v[4][D / 64];  // rows 4*quad .. 4*quad+3
+  uint32_t kmask;
+};
+
+// Two e4m3 values, in the lower or the upper half of a word, as two bf16 values.
+template <bool HI>
+__device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, HI));
+}
+
 // Columns of the score tile per copy of the query heads (column n carries head n % kCopy<G>).
 template <int G>
 constexpr int kCopy = G <= 4 ? 4 : 8;
@@ -191,6 +216,33 @@ __device__ __forceinline__ void load_page_tile(Tile<D>& t, const uint16_t* kt, c
   }
 }
 
+// The same for an e4m3 cache (kt, vt: byte addresses).
+template <int D>
+__device__ __forceinline__ void load_page_tile(Tile8<D>& t, const uint8_t* kt, const uint8_t* vt,
+                                               bool real, int lane) {
+  using G8 = Geo8<D>;
+  const int quad = lane >> 4, hcol = lane & 15;
+  const int bytes = real ? 16 * D : 0;
+  const __amdgpu_buffer_rsrc_t rk =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(kt), 0, bytes, kRawBufferFlags);
+  const __amdgpu_buffer_rsrc_t rv =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(vt), 0, bytes, kRawBufferFlags);
+  const int ko = 16 * lane, vo = quad * 4 * D + Geo<D>::NC * hcol;
+#pragma unroll
+  for (int i = 0; i < G8::NL; ++i)
+    t.k[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, ko + 1024 * i, 0, kNonTemporal));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (D == 128) {
+      const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rv, vo + D * i, 0, kNonTemporal));
+      t.v[i][0] = w[0];
+      t.v[i][1] = w[1];
+    } else {
+      t.v[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rv, vo + D * i, 0, kNonTemporal);
+    }
+  }
+}
+
 // 16-byte piece c of row r of a K tile in the wave's LDS slice (16 * D bf16): the pieces of a row
 // are permuted by the row, so that 16 lanes reading the same piece of 16 rows touch all 64 banks
 // (d = 128: 256-byte rows; d = 64: two rows per 256 bytes).
@@ -212,6 +264,40 @@ __device__ __forceinline__ void k_operand(const Tile<D>& t, uint16_t* lk, u32x4 
 #pragma unroll
   for (int ks = 0; ks < Gm::NK; ++ks)
     ka[ks] = *reinterpret_cast<const u32x4*>(lk + k_slot<D>(lane & 15, 4 * ks + (lane >> 4)));
+}
+
+// The same from an e4m3 tile: each 16-byte piece of a row becomes two of the bf16 row.
+template <int D>
+__device__ __forceinline__ void k_operand(const Tile8<D>& t, uint16_t* lk, u32x4 (&ka)[Geo<D>::NK],
+                                          int lane) {
+  using G8 = Geo8<D>;
+  wave_lds_sync();
+#pragma unroll
+  for (int i = 0; i < G8::NL; ++i) {
+    const int r = G8::RPL * i + lane / G8::CPR, c = 2 * (lane % G8::CPR);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const u32x4 w = {e4m3x2_to_bf16x2<false>(t.k[i][2 * j]), e4m3x2_to_bf16x2<true>(t.k[i][2 * j]),
+                       e4m3x2_to_bf16x2<false>(t.k[i][2 * j + 1]), e4m3x2_to_bf16x2<true>(t.k[i][2 * j + 1])};
+      *reinterpret_cast<u32x4*>(lk + k_slot<D>(r, c + j)) = w;
+    }
+  }
+  wave_lds_sync();
+#pragma unroll
+  for (int ks = 0; ks < Geo<D>::NK; ++ks)
+    ka[ks] = *reinterpret_cast<const u32x4*>(lk + k_slot<D>(lane & 15, 4 * ks + (lane >> 4)));
+}
+
+// The V columns of an e4m3 tile in the layout of a bf16 tile.
+template <int D>
+__device__ __forceinline__ void expand_v(const Tile8<D>& raw, Tile<D>& t) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int w = 0; w < D / 64; ++w) {
+      t.v[i][2 * w] = e4m3x2_to_bf16x2<false>(raw.v[i][w]);
+      t.v[i][2 * w + 1] = e4m3x2_to_bf16x2<true>(raw.v[i][w]);
+    }
 }
 
 // Folds one tile's score tile (acc: lane (quad, hcol) holds q_(hcol % S) . k_r for rows
@@ -316,6 +402,24 @@ __device__ __forceinline__ void process_tile(Tile<D>& t, const bf16x8 (&qb)[Geo<
                                              uint16_t* lk, float* logit_slot, int lane) {
   u32x4 ka[Geo<D>::NK];
   k_operand<D>(t, lk, ka, lane);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int ks = 0; ks < Geo<D>::NK; ++ks)
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[ks]), qb[ks],
+                                                  acc, 0, 0, 0);
+  fold_tile<D, G, LOGITS>(acc, t, scale_log2, st, logit_slot, lane);
+}
+
+// The same for a tile of an e4m3 cache (scale_log2 includes the KV head's K scale).
+template <int D, int G, bool LOGITS>
+__device__ __forceinline__ void process_tile(Tile8<D>& raw, const bf16x8 (&qb)[Geo<D>::NK],
+                                             float scale_log2, WaveSoftmax<D, G>& st,
+                                             uint16_t* lk, float* logit_slot, int lane) {
+  u32x4 ka[Geo<D>::NK];
+  k_operand<D>(raw, lk, ka, lane);
+  Tile<D> t;
+  t.kmask = raw.kmask;
+  expand_v<D>(raw, t);
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int ks = 0; ks < Geo<D>::NK; ++ks)

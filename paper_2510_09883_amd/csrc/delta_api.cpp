@@ -13,6 +13,7 @@
 #include <mutex>
 
 #include "../../include/delta_attn.h"
+#include "api_common.h"
 #include "internal.h"
 
 namespace {
@@ -20,11 +21,6 @@ namespace {
 using namespace delta;
 
 static_assert(kNoallocScratchBytes == DELTA_NOALLOC_SCRATCH_BYTES, "scratch size of the C ABI");
-
-constexpr size_t kAlign = 256;
-
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // Workgroups the attention launch aims for: about one per CU (256 CUs).  Measured on MI355X,
 // more and shorter workgroups (up to 4096) were slower at every workload size: each one pays a
@@ -155,22 +151,6 @@ struct Layout {
   RowMode sparse_mode = ROWS_SEL_PAGE;
 };
 
-int check_shape(const delta_shape_t* s) {
-  if (!s) return DELTA_ERR_INVALID_ARG;
-  if (s->batch < 1 || s->n_q_heads < 1 || s->n_kv_heads < 1 || s->max_seq_len < 1 ||
-      s->max_pages_per_seq < 1 || !(s->sm_scale >= 0.f) || isinf(s->sm_scale))
-    return DELTA_ERR_INVALID_ARG;
-  if (s->n_q_heads % s->n_kv_heads != 0) return DELTA_ERR_INVALID_ARG;
-  if ((int64_t)s->max_seq_len > (int64_t)s->max_pages_per_seq * 16) return DELTA_ERR_INVALID_ARG;
-  if (s->page_size != 16) return DELTA_ERR_UNSUPPORTED;
-  if (s->head_dim != 64 && s->head_dim != 128) return DELTA_ERR_UNSUPPORTED;
-  const int G = s->n_q_heads / s->n_kv_heads;
-  if (G > kMaxGroup) return DELTA_ERR_UNSUPPORTED;
-  if ((int64_t)s->batch * s->n_q_heads > (1 << 24) || s->batch > 65535 || s->n_kv_heads > 65535)
-    return DELTA_ERR_UNSUPPORTED;
-  return DELTA_OK;
-}
-
 // The recency window in units.  App. A, Alg. 1 keeps the last ceil(L / P) pages for a window
 // of L tokens, so any token count is valid: the window is the last ceil(l / U) units.
 int recent_units_of(const delta_select_t* sel) {
@@ -239,22 +219,13 @@ int make_layout(const delta_shape_t* s, const delta_select_t* sel, Layout* L) {
   return DELTA_OK;
 }
 
-int check_kv(const delta_kv_t* kv) {
-  if (!kv || !kv->k_cache || !kv->v_cache || !kv->page_table || !kv->seq_lens || kv->n_pages < 0)
-    return DELTA_ERR_INVALID_ARG;
-  return DELTA_OK;
-}
-
-float scale_log2(const delta_shape_t* s) {
-  const float sc = s->sm_scale > 0.f ? s->sm_scale : 1.0f / sqrtf((float)s->head_dim);
-  return sc * 1.4426950408889634f;
-}
-
 AttnArgs base_args(const delta_shape_t* s, const delta_kv_t* kv, const void* q, void* out,
                    const Layout& L, char* ws, const SplitPlan& plan) {
   AttnArgs a{};
   a.k_cache = static_cast<const uint16_t*>(kv->k_cache);
   a.v_cache = static_cast<const uint16_t*>(kv->v_cache);
+  a.k_scale = kv->k_scale;
+  a.v_scale = kv->v_scale;
   a.page_table = kv->page_table;
   a.seq_lens = kv->seq_lens;
   a.q = static_cast<const uint16_t*>(q);
@@ -281,12 +252,10 @@ AttnArgs base_args(const delta_shape_t* s, const delta_kv_t* kv, const void* q, 
   return a;
 }
 
-int hip_rc(hipError_t e) { return e == hipSuccess ? DELTA_OK : DELTA_ERR_HIP; }
-
 int run_full(const delta_shape_t* s, const delta_kv_t* kv, const void* q, void* out,
              const Layout& L, char* ws, hipStream_t st) {
   AttnArgs a = base_args(s, kv, q, out, L, ws, L.dense);
-  return hip_rc(launch_attention(s->head_dim, s->n_q_heads / s->n_kv_heads, ROWS_DENSE, a,
+  return hip_rc(launch_attention(s->head_dim, s->n_q_heads / s->n_kv_heads, ROWS_DENSE, is_e4m3(kv), a,
                                  s->batch, st));
 }
 
@@ -359,7 +328,7 @@ int run_delta(const delta_shape_t* s, const delta_kv_t* kv, const void* q, void*
   xa.unit_tokens = sel->unit_tokens;
   xa.budget_units = sel->budget_tokens / sel->unit_tokens;
   xa.recent_units = recent_units_of(sel);
-  if (use_fused_delta(s, sel, L)) {
+  if (!is_e4m3(kv) && use_fused_delta(s, sel, L)) {   // (the fused kernel reads bf16)
     FusedArgs f{};
     f.k_cache = static_cast<const uint16_t*>(kv->k_cache);
     f.v_cache = static_cast<const uint16_t*>(kv->v_cache);
@@ -391,7 +360,7 @@ int run_delta(const delta_shape_t* s, const delta_kv_t* kv, const void* q, void*
   AttnArgs a = base_args(s, kv, q, out, L, ws, L.dense);
   a.logits = reinterpret_cast<float*>(ws + L.logits);
   a.lse = reinterpret_cast<float*>(ws + L.lse);
-  int rc = hip_rc(launch_attention(s->head_dim, s->n_q_heads / s->n_kv_heads, ROWS_DENSE, a,
+  int rc = hip_rc(launch_attention(s->head_dim, s->n_q_heads / s->n_kv_heads, ROWS_DENSE, is_e4m3(kv), a,
                                    s->batch, st));
   if (rc) return rc;
   ScoreArgs sa{};
@@ -419,7 +388,7 @@ int run_sparse(const delta_shape_t* s, const delta_kv_t* kv, const void* q, void
   a.sel_cnt = sel_cnt;
   a.sel_phys = phys;
   a.sel_stride = sel->budget_tokens / sel->unit_tokens;
-  return hip_rc(launch_attention(s->head_dim, s->n_q_heads / s->n_kv_heads, L.sparse_mode, a,
+  return hip_rc(launch_attention(s->head_dim, s->n_q_heads / s->n_kv_heads, L.sparse_mode, is_e4m3(kv), a,
                                  s->batch, st));
 }
 

@@ -36,8 +36,10 @@ constexpr int kBalanceMaxBatch = 64;     // sequences of a balanced launch (one 
 constexpr int kCounterStride = 64;
 
 struct AttnArgs {
-  const uint16_t* k_cache;   // bf16 [pages, Hkv, 16, D]
+  const uint16_t* k_cache;   // bf16 [pages, Hkv, 16, D], or e4m3 (kv8)
   const uint16_t* v_cache;
+  const float* k_scale;      // [Hkv] of an e4m3 cache, or null (1)
+  const float* v_scale;
   const int32_t* page_table; // [B, max_pages]
   const int32_t* seq_lens;   // [B]
   const int32_t* sel_idx;    // [B, sel_stride] (sparse modes)
@@ -65,7 +67,7 @@ struct AttnArgs {
   uint32_t* status;          // debug status word (workspace byte 0)
 };
 
-hipError_t launch_attention(int head_dim, int group, int mode, const AttnArgs& a, int batch,
+hipError_t launch_attention(int head_dim, int group, int mode, bool kv8, const AttnArgs& a, int batch,
                             hipStream_t stream);
 
 struct ScoreArgs {

@@ -25,6 +25,7 @@ DELTA_ERR_HOOK = -5
 DELTA_ROLE_FULL, DELTA_ROLE_DELTA, DELTA_ROLE_SPARSE = 0, 1, 2
 DELTA_AGG_MAX, DELTA_AGG_SUM = 0, 1
 DELTA_PATH_AUTO, DELTA_PATH_SPLIT, DELTA_PATH_FUSED = 0, 1, 2
+DELTA_KV_BF16, DELTA_KV_E4M3 = 0, 1
 
 EXPORTED = ["delta_workspace_bytes", "delta_workspace_init", "delta_full_attn",
             "delta_delta_attn_select", "delta_sparse_attn", "delta_decode_step",
@@ -45,7 +46,8 @@ class delta_shape_t(ctypes.Structure):
 class delta_kv_t(ctypes.Structure):
     _fields_ = [("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p),
                 ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
-                ("n_pages", ctypes.c_int64)]
+                ("n_pages", ctypes.c_int64), ("kv_type", ctypes.c_int32),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
 class delta_select_t(ctypes.Structure):
@@ -155,10 +157,13 @@ def _check_kv(kv, shape):
     t = getattr(kv, "_tensors", None)
     if t is None:   # built by hand from raw pointers: nothing to check
         return
-    k, v, pt, sl = t
+    k, v, pt, sl, scales = t
     cache = (None, shape.n_kv_heads, shape.page_size, shape.head_dim)
-    _dev("k_cache", k, torch.bfloat16, cache)
-    _dev("v_cache", v, torch.bfloat16, cache)
+    kind = torch.float8_e4m3fn if kv.kv_type == DELTA_KV_E4M3 else torch.bfloat16
+    _dev("k_cache", k, kind, cache)
+    _dev("v_cache", v, kind, cache)
+    for name, s in scales:
+        _dev(name, s, torch.float32, (shape.n_kv_heads,))
     _dev("page_table", pt, torch.int32, (shape.batch, shape.max_pages_per_seq))
     _dev("seq_lens", sl, torch.int32, (shape.batch,))
 
@@ -192,16 +197,22 @@ def make_select(budget_tokens, recent_tokens, unit_tokens=16, agg=DELTA_AGG_MAX,
     return delta_select_t(budget_tokens, recent_tokens, unit_tokens, agg, delta_path)
 
 
-def make_kv(k_cache, v_cache, page_table, seq_lens) -> delta_kv_t:
+def make_kv(k_cache, v_cache, page_table, seq_lens, k_scale=None, v_scale=None) -> delta_kv_t:
+    """One layer's cache.  Caches of torch.float8_e4m3fn may have a float32 scale per KV head
+    (k_scale, v_scale; None: 1)."""
     for name, t in (("k_cache", k_cache), ("v_cache", v_cache), ("page_table", page_table),
                     ("seq_lens", seq_lens)):
         _dev(name, t)
     if k_cache.dim() < 1 or v_cache.dim() < 1 or k_cache.shape[0] != v_cache.shape[0]:
         raise ValueError(f"k_cache and v_cache must hold the same number of pages "
                          f"(got {tuple(k_cache.shape)}, {tuple(v_cache.shape)})")
+    e4m3 = k_cache.dtype == torch.float8_e4m3fn
+    scales = [(n, _dev(n, t)) for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if t is not None]
+    if scales and not e4m3:
+        raise ValueError(f"{scales[0][0]}: only caches of torch.float8_e4m3fn have scales")
     kv = delta_kv_t(k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
-                    k_cache.shape[0])
-    kv._tensors = (k_cache, v_cache, page_table, seq_lens)   # checked against the shape per call
+                    k_cache.shape[0], DELTA_KV_E4M3 if e4m3 else DELTA_KV_BF16, _ptr(k_scale), _ptr(v_scale))
+    kv._tensors = (k_cache, v_cache, page_table, seq_lens, scales)   # checked against the shape per call
     return kv
 
 
@@ -304,7 +315,7 @@ class StepArgs:
         self.outs = (_vp * n)(*[o.data_ptr() for o in outs])
         self.sel = sel
         self.sel_idx, self.sel_cnt, self.ws = sel_idx, sel_cnt, ws
-        self._keep = (qs, outs)
+        self._keep = (qs, outs, list(kvs))
 
 
 def delta_decode_step(args: StepArgs):
@@ -326,6 +337,7 @@ def delta_decode_step_noalloc(args: StepArgs):
 
 
 def delta_kv_append(shape, k_cache, v_cache, page_table, seq_lens, k_new, v_new):
+    _dev("k_cache", k_cache, torch.bfloat16)   # (e4m3 caches: extend.delta_rope_append)
     _check_kv(make_kv(k_cache, v_cache, page_table, seq_lens), shape)
     row = (shape.batch, shape.n_kv_heads, shape.head_dim)
     _dev("k_new", k_new, torch.bfloat16, row)
