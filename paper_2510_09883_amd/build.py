@@ -19,6 +19,7 @@ DEBUG_LIB = os.path.join(PKG, "libdelta_attn_debug.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["attn_kernel.hip", "fused_delta_kernel.hip", "select_kernel.hip", "append_kernel.hip",
+           "rope_append_kernel.hip", "extend_kernel.hip", "extend_api.cpp",
            "probe_kernel.hip", "noalloc.hip", "delta_api.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-mcode-object-version=5",

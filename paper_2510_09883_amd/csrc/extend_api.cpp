@@ -1,0 +1,169 @@
+// C ABI of the prompt side (include/delta_extend.h): argument checks, the cut of a call into tiles
+// and splits, the workspace layout, and the launches.
+#include <algorithm>
+
+#include "api_common.h"
+#include "extend.h"
+
+namespace delta {
+
+// Tiles of 32 rows while a run fits one, of 256 otherwise; splits along the cache while the tiles
+// alone leave CUs idle.  From host-side bounds alone.
+ExtendPlan plan_extend(const delta_shape_t* s, int n_rows, int max_new) {
+  ExtendPlan p;
+  const int G = s->n_q_heads / s->n_kv_heads;
+  p.rows = (int64_t)max_new * G <= 32 ? 32 : 256;
+  // every run ends in a partial tile: at most one more tile per run than whole ones
+  const int64_t by_run = (int64_t)s->batch * (((int64_t)max_new * G + p.rows - 1) / p.rows);
+  const int64_t by_row = (int64_t)n_rows * G / p.rows + std::min(s->batch, n_rows);
+  p.tiles = (int)std::min(by_run, by_row);
+  const int64_t wgs = std::max<int64_t>(1, (int64_t)p.tiles * s->n_kv_heads);
+  const int64_t want = (256 + wgs - 1) / wgs, most = std::max(1, ceil_div(s->max_seq_len, 512));
+  p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 32}));
+  return p;
+}
+
+}  // namespace delta
+
+namespace {
+
+using namespace delta;
+
+bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int check_runs(const delta_shape_t* s, int32_t n_rows, const int32_t* row_offsets) {
+  if (n_rows < 0) return DELTA_ERR_INVALID_ARG;
+  if (!row_offsets && n_rows != s->batch) return DELTA_ERR_INVALID_ARG;
+  if ((int64_t)n_rows * s->n_q_heads > (1 << 28)) return DELTA_ERR_UNSUPPORTED;
+  return DELTA_OK;
+}
+
+Runs runs_of(const delta_shape_t* s, const delta_kv_t* kv, int32_t n_rows, const int32_t* row_offsets) {
+  return Runs{row_offsets, kv->seq_lens, kv->page_table, n_rows, s->batch, s->max_pages_per_seq};
+}
+
+struct ExtendLayout {
+  ExtendPlan plan;
+  size_t status = 0, part_ml = 0, part_o = 0, total = 0;
+};
+
+int extend_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, ExtendLayout* L) {
+  int rc = check_shape(s);
+  if (rc) return rc;
+  if (n_rows < 0 || max_new < 0 || max_new > n_rows) return DELTA_ERR_INVALID_ARG;
+  if ((int64_t)n_rows * s->n_q_heads > (1 << 28)) return DELTA_ERR_UNSUPPORTED;
+  L->plan = plan_extend(s, n_rows, max_new);
+  if (L->plan.tiles > 65535) return DELTA_ERR_UNSUPPORTED;
+  size_t off = 0;
+  L->status = off; off = align_up(off + sizeof(uint32_t));
+  if (L->plan.n_split > 1) {
+    const size_t parts = (size_t)L->plan.n_split * n_rows * s->n_q_heads;
+    L->part_ml = off; off = align_up(off + sizeof(float) * 2 * parts);
+    L->part_o = off;  off = align_up(off + sizeof(float) * s->head_dim * parts);
+  }
+  L->total = off;
+  return DELTA_OK;
+}
+
+}  // namespace
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+int delta_rope_append(const delta_shape_t* shape, const delta_kv_t* kv, const delta_rope_t* rope,
+                      int32_t n_rows, const int32_t* row_offsets, const void* q,
+                      int64_t q_row_stride, const void* k, int64_t k_row_stride, const void* v,
+                      int64_t v_row_stride, void* q_out, void* stream) {
+  int rc = check_shape(shape);
+  if (rc) return rc;
+  if ((rc = check_kv(kv))) return rc;
+  if ((rc = check_runs(shape, n_rows, row_offsets))) return rc;
+  if (rope) {
+    if (!rope->inv_freq || rope->rotary_dim < 16 || rope->rotary_dim > shape->head_dim ||
+        rope->rotary_dim % 16 || (rope->interleaved != 0 && rope->interleaved != 1))
+      return DELTA_ERR_INVALID_ARG;
+  }
+  if (n_rows == 0) return DELTA_OK;
+  if (!k || !v || !q != !q_out) return DELTA_ERR_INVALID_ARG;
+  const int64_t q_row = (int64_t)shape->n_q_heads * shape->head_dim;
+  const int64_t kv_row = (int64_t)shape->n_kv_heads * shape->head_dim;
+  if (k_row_stride < kv_row || k_row_stride % 8 || v_row_stride < kv_row || v_row_stride % 8 ||
+      (q && (q_row_stride < q_row || q_row_stride % 8)))
+    return DELTA_ERR_INVALID_ARG;
+  for (const void* p : {q, k, v, static_cast<const void*>(q_out), kv->k_cache, kv->v_cache})
+    if (!aligned(p, 16)) return DELTA_ERR_INVALID_ARG;
+  RopeAppendArgs a{};
+  a.runs = runs_of(shape, kv, n_rows, row_offsets);
+  // (the cache descriptor is shared with the calls that only read it)
+  a.k_cache = static_cast<uint8_t*>(const_cast<void*>(kv->k_cache));
+  a.v_cache = static_cast<uint8_t*>(const_cast<void*>(kv->v_cache));
+  a.k_scale = kv->k_scale;
+  a.v_scale = kv->v_scale;
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.q_stride = q_row_stride;
+  a.k_stride = k_row_stride;
+  a.v_stride = v_row_stride;
+  a.page_stride = (int64_t)shape->n_kv_heads * 16 * shape->head_dim;
+  if (rope) {
+    a.inv_freq = rope->inv_freq;
+    a.positions = rope->positions;
+    a.rotary_dim = rope->rotary_dim;
+    a.interleaved = rope->interleaved;
+  }
+  a.n_q_heads = q ? shape->n_q_heads : 0;
+  a.n_kv_heads = shape->n_kv_heads;
+  a.n_pages = kv->n_pages;
+  return hip_rc(launch_rope_append(shape->head_dim, is_e4m3(kv), a, static_cast<hipStream_t>(stream)));
+}
+
+int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int32_t max_new, size_t* out) {
+  if (!out) return DELTA_ERR_INVALID_ARG;
+  ExtendLayout L;
+  int rc = extend_layout(shape, n_rows, max_new, &L);
+  if (rc) return rc;
+  *out = L.total;
+  return DELTA_OK;
+}
+
+int delta_extend_attn(const delta_shape_t* shape, const delta_kv_t* kv, int32_t n_rows,
+                      int32_t max_new, const int32_t* row_offsets, const void* q, void* out,
+                      void* ws, size_t ws_bytes, void* stream) {
+  ExtendLayout L;
+  int rc = extend_layout(shape, n_rows, max_new, &L);
+  if (rc) return rc;
+  if ((rc = check_kv(kv))) return rc;
+  if ((rc = check_runs(shape, n_rows, row_offsets))) return rc;
+  if (!row_offsets && max_new < 1) return DELTA_ERR_INVALID_ARG;
+  if (!ws) return DELTA_ERR_INVALID_ARG;
+  if (ws_bytes < L.total) return DELTA_ERR_WORKSPACE;
+  if (n_rows == 0 || max_new == 0) return DELTA_OK;
+  if (!q || !out) return DELTA_ERR_INVALID_ARG;
+  for (const void* p : {q, static_cast<const void*>(out), kv->k_cache, kv->v_cache})
+    if (!aligned(p, 16)) return DELTA_ERR_INVALID_ARG;
+  if (!aligned(ws, 256)) return DELTA_ERR_INVALID_ARG;
+  char* w = static_cast<char*>(ws);
+  ExtendArgs a{};
+  a.runs = runs_of(shape, kv, n_rows, row_offsets);
+  a.k_cache = static_cast<const uint8_t*>(kv->k_cache);
+  a.v_cache = static_cast<const uint8_t*>(kv->v_cache);
+  a.k_scale = kv->k_scale;
+  a.v_scale = kv->v_scale;
+  a.q = static_cast<const uint16_t*>(q);
+  a.out = static_cast<uint16_t*>(out);
+  a.part_ml = reinterpret_cast<float*>(w + L.part_ml);
+  a.part_o = reinterpret_cast<float*>(w + L.part_o);
+  a.page_stride = (int64_t)shape->n_kv_heads * 16 * shape->head_dim;
+  a.n_q_heads = shape->n_q_heads;
+  a.n_kv_heads = shape->n_kv_heads;
+  a.n_split = L.plan.n_split;
+  a.scale_log2 = scale_log2(shape);
+  a.n_pages = kv->n_pages;
+  a.status = reinterpret_cast<uint32_t*>(w + L.status);
+  return hip_rc(launch_extend(L.plan, shape->head_dim, is_e4m3(kv), a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+#pragma GCC visibility pop

@@ -1,0 +1,397 @@
+// Causal attention of runs of new tokens over the paged cache (Sec. 2, Eq. gqa_attention, for more
+// than one query token of a sequence).
+//
+// Mathematics.  A row is one (new token, query head) pair.  out = sum_t p_t v_t / sum_t p_t over the
+// tokens t the row sees, p_t = 2^(s_t - m), s_t the scaled score in the log2 domain, m the running
+// maximum: one pass over the keys, the sums rescaled when the maximum rises (Milakov and Gimelshein,
+// "Online normalizer calculation for softmax", 2018).
+//
+// Work.  The rows of a run that share a KV head (token-major, the group's query heads next to each
+// other) are cut into tiles; a workgroup takes a tile, and one of n_split pieces of the keys that
+// the tile's last row sees.  It walks them in blocks that all its waves bring to LDS, 16 bytes a
+// thread and load, the next block's loads in flight (in registers) while one is worked on.  A wave
+// holds 32 rows and takes 32*KT keys of a block; WR waves stand along the rows, WK along the keys.
+//
+//   * S^T = K Q^T by v_mfma_f32_32x32x16_bf16 with A = 32 keys, B = the 32 rows' queries (in
+//     registers throughout).  Lane (h, n) = (lane / 32, lane % 32) gets row n's scores of keys
+//     8*(i/4) + 4*h + i%4, i = 0 .. 15: a row lives in two lanes, so that its maximum and sum are
+//     formed in registers and one swap of the wave's halves.
+//   * O^T = V^T P^T by the same instruction.  Its B operand wants row n's probabilities of 8 keys
+//     in lane (h, n), which is what the lane holds: keys 16*s + 4*h + {0..3} and 16*s + 8 + 4*h +
+//     {0..3}.  The order of the keys in a contraction is free as long as A has the same one: V
+//     comes from LDS by ds_read_b64_tr_b16, which hands 4 consecutive keys of one element to a
+//     lane, once for each four.  No probability changes its lane.
+//
+// LDS layouts: K rows with their 16-byte pieces permuted by the row (16 lanes reading one piece of
+// 16 rows touch all banks), V rows with their 64-byte pieces permuted by the row (the four rows of
+// a transposing read do).
+#include <type_traits>
+
+#include "attn_tile.h"
+#include "debug_check.h"
+#include "runs.h"
+
+namespace delta {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+
+// Element offset of 8-element piece c of row r of the K block.
+template <int D>
+__device__ __forceinline__ int k_at(int r, int c) {
+  return r * D + 8 * (c ^ (D == 128 ? r & 15 : (r >> 1) & 7));
+}
+// Element offset of element e of row r of the V block.
+template <int D>
+__device__ __forceinline__ int v_at(int r, int e) {
+  return r * D + (e ^ (D == 128 ? (r & 3) << 5 : ((r >> 1) & 1) << 5));
+}
+
+template <int D, int WR, int WK, int KT, bool KV8>
+__global__ __launch_bounds__(64 * WR * WK, 1) void extend_kernel(const ExtendArgs a) {
+  constexpr int NW = WR * WK, T = 64 * NW;
+  constexpr int BM = 32 * WR;           // rows of a tile
+  constexpr int BK = 32 * KT;           // keys a wave takes of a block
+  constexpr int BN = BK * WK;           // keys of a block
+  constexpr int NK = D / 16;            // MFMA steps of a score tile
+  constexpr int ND = D / 32;            // 32-element parts of an output row
+  constexpr int EB = KV8 ? 1 : 2;       // bytes of a cache element
+  constexpr int CPR = D * EB / 16;      // 16-byte pieces of a cache row
+  constexpr int kPieces = BN * CPR;     // of a block, of K and of V
+  constexpr int NL = (kPieces + T - 1) / T;   // loads per thread and block (the last waves may have none)
+  constexpr int RPW = 64 / CPR;         // rows of a wave-wide load
+  static_assert(kPieces % 64 == 0 && 16 % RPW == 0, "whole loads, each inside one page");
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = wave % WR, wk = wave / WR;
+  const int n = lane & 31, h = lane >> 5;
+  const int g = blockIdx.x, split = blockIdx.z;
+  const int Hq = a.n_q_heads, G = Hq / a.n_kv_heads;
+
+  constexpr int kBlock = BN * D;        // elements of a K or V block
+  constexpr int kMerge = WK > 1 ? (WK - 1) * WR * 64 * (16 * ND + 2) * 2 : 0;   // (in 16-bit units)
+  constexpr int kLds = 4 * kBlock > kMerge ? 4 * kBlock : kMerge;
+  __shared__ __attribute__((aligned(256))) uint16_t s_kv[kLds];   // K, V of two blocks; then the merge
+
+  // ---- the tile: which sequence, which of its rows ----------------------------------------
+  int tile = blockIdx.y, b = 0, begin = 0, n_new = 0;
+  bool found = false;
+  for (int c = 0; c < a.runs.batch && !found; c += 64) {
+    int lo = 0, len = 0;
+    if (c + lane < a.runs.batch) {
+      lo = run_offset(a.runs, c + lane);
+      len = max(0, run_offset(a.runs, c + lane + 1) - lo);
+    }
+    const int tiles = (int)(((int64_t)len * G + BM - 1) / BM);
+    const int incl = wave_incl_scan(tiles);
+    const uint64_t past = __ballot(incl > tile);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      b = c + l;
+      begin = __builtin_amdgcn_readlane(lo, l);
+      n_new = __builtin_amdgcn_readlane(len, l);
+      const int mine = __builtin_amdgcn_readlane(tiles, l);
+      tile -= __builtin_amdgcn_readlane(incl, l) - mine;
+      tile = mine - 1 - tile;   // the last rows see most keys: they start first
+      found = true;
+    } else {
+      tile -= __builtin_amdgcn_readlane(incl, 63);
+    }
+  }
+  if (!found) return;
+  const int s_b = max(0, min(a.runs.seq_lens[b], 16 * a.runs.max_pages));
+  const int n_tile_rows = n_new * G;    // (n_rows * Hq < 2^31)
+  // this lane's row: token j of the run, query head g * G + head
+  const int r0 = tile * BM + 32 * wr;
+  const int r = min(r0 + n, n_tile_rows - 1);
+  const bool real = r0 + n < n_tile_rows;
+  const int j = r / G, head = g * G + (r - j * G);
+  const size_t out_row = (size_t)(begin + j) * Hq + head;
+  const int lim = max(0, s_b - n_new + j + 1);                        // keys the row sees
+  auto lim_of = [&](int row) { return max(0, s_b - n_new + min(row, n_tile_rows - 1) / G + 1); };
+  const int lim_lo = lim_of(r0), lim_hi = lim_of(r0 + 31);            // of the wave's rows
+  const int lim_tile = lim_of(tile * BM + BM - 1);
+
+  const int n_blocks = (lim_tile + BN - 1) / BN;
+  const int per_split = (n_blocks + a.n_split - 1) / a.n_split;
+  const int blk0 = split * per_split, blk1 = min(n_blocks, blk0 + per_split);
+
+  const float scale = KV8 && a.k_scale ? a.scale_log2 * a.k_scale[g] : a.scale_log2;
+  bf16x8 q[NK];
+#pragma unroll
+  for (int ks = 0; ks < NK; ++ks)
+    q[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(a.q + out_row * D + 16 * ks + 8 * h));
+
+  float m = kNegInfF, l = 0.f;
+  f32x16 o[ND];
+#pragma unroll
+  for (int i = 0; i < ND; ++i) o[i] = f32x16{};
+
+  // ---- blocks: pages of the next 64 (one per lane), loads, LDS ------------------------------
+  const int32_t* table = a.runs.page_table + (size_t)b * a.runs.max_pages;
+  const int last_page = max(0, (s_b - 1) >> 4);
+  int page_base = blk0 * BN / 16;
+  int pages = 0;
+  auto list_pages = [&](int base) {
+    pages = checked_page(table[min(base + lane, last_page)], a.n_pages, a.status);
+    page_base = base;
+  };
+  u32x4 kr[NL], vr[NL];
+  auto load = [&](int blk) {
+    const int first = blk * BN / 16;
+    if (first + BN / 16 > page_base + 64) list_pages(first);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = (i * NW + wave) * RPW;   // the wave's first row of this load, in the block
+      if (kPieces % T && row >= BN) break;
+      const int page = __builtin_amdgcn_readlane(pages, first + row / 16 - page_base);
+      const size_t at = ((size_t)page * a.page_stride + (size_t)(g * 16 + row % 16) * D) * EB + 16 * lane;
+      kr[i] = *reinterpret_cast<const u32x4*>(a.k_cache + at);
+      vr[i] = *reinterpret_cast<const u32x4*>(a.v_cache + at);
+    }
+  };
+  auto store = [&](int blk, int buf) {
+    uint16_t* sk = s_kv + buf * 2 * kBlock;
+    uint16_t* sv = sk + kBlock;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = (i * NW + wave) * RPW + lane / CPR, c = lane % CPR;
+      if (kPieces % T && row >= BN) break;
+      u32x4 v = vr[i];
+      // rows past the sequence: 0 times what they hold (NaN) would spoil the sums
+      if (blk * BN + row >= s_b) v = u32x4{0u, 0u, 0u, 0u};
+      if constexpr (KV8) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          u32x4 wk, wv;
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            wk[2 * w] = e4m3x2_to_bf16x2<false>(kr[i][2 * half + w]);
+            wk[2 * w + 1] = e4m3x2_to_bf16x2<true>(kr[i][2 * half + w]);
+            wv[2 * w] = e4m3x2_to_bf16x2<false>(v[2 * half + w]);
+            wv[2 * w + 1] = e4m3x2_to_bf16x2<true>(v[2 * half + w]);
+          }
+          *reinterpret_cast<u32x4*>(sk + k_at<D>(row, 2 * c + half)) = wk;
+          *reinterpret_cast<u32x4*>(sv + v_at<D>(row, 16 * c + 8 * half)) = wv;
+        }
+      } else {
+        *reinterpret_cast<u32x4*>(sk + k_at<D>(row, c)) = kr[i];
+        *reinterpret_cast<u32x4*>(sv + v_at<D>(row, 8 * c)) = v;
+      }
+    }
+  };
+
+  auto attend = [&](int blk, int buf) {
+    const int key0 = blk * BN + wk * BK;   // the wave's first key
+    if (key0 >= lim_hi) return;
+    const uint16_t* sk = s_kv + buf * 2 * kBlock + wk * BK * D;
+    const uint16_t* sv = s_kv + buf * 2 * kBlock + kBlock + wk * BK * D;
+    f32x16 s[KT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      s[kt] = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) {
+        const bf16x8 ka = __builtin_bit_cast(
+            bf16x8, *reinterpret_cast<const u32x4*>(sk + k_at<D>(32 * kt + n, 2 * ks + h)));
+        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, q[ks], s[kt], 0, 0, 0);
+      }
+    }
+    {
+// a scaled score is rounded before the maximum and the difference see it: contracted into the
+// difference's fma, the maximum's own rounding error would be left in the exponent
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) s[kt] *= scale;
+      if (key0 + BK > lim_lo) {   // some row of the wave does not see all of these keys
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = key0 + 32 * kt + 8 * (i / 4) + 4 * h + i % 4;
+            s[kt][i] = key < lim ? s[kt][i] : kNegInfF;
+          }
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
+      mx = max_xor32(mx);
+      if (__any(mx > m)) {
+        const float m_new = fmaxf(m, mx);
+        const float alpha = __builtin_amdgcn_exp2f(m - (m_new == kNegInfF ? 0.f : m_new));
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] *= alpha;
+      }
+      const float m_use = m == kNegInfF ? 0.f : m;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[kt][i] = __builtin_amdgcn_exp2f(s[kt][i] - m_use);
+          l += s[kt][i];
+        }
+    }
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        u32x4 pw;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const bf16x2 p = {(__bf16)s[kt][8 * st + 2 * w], (__bf16)s[kt][8 * st + 2 * w + 1]};
+          pw[w] = __builtin_bit_cast(uint32_t, p);
+        }
+        const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          // lane i of 16 names key i / 4 of four, elements 4 * (i % 4); it gets element i of all four
+          const int row = 32 * kt + 16 * st + 4 * h + (lane & 15) / 4;
+          const int e = 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+          const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(sv + v_at<D>(row, e)));
+          const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(sv + v_at<D>(row + 8, e)));
+          typedef short i16x8 __attribute__((ext_vector_type(8)));
+          const i16x8 va = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), pb, o[d], 0, 0, 0);
+        }
+      }
+  };
+
+  // ---- the walk ---------------------------------------------------------------------------
+  if (blk0 < blk1) {
+    list_pages(page_base);
+    load(blk0);
+    store(blk0, 0);
+    for (int blk = blk0; blk < blk1; ++blk) {
+      const int buf = (blk - blk0) & 1;
+      const bool more = blk + 1 < blk1;
+      if (more) load(blk + 1);
+      lds_barrier();   // the block is in LDS, and nobody reads the other buffer any more
+      attend(blk, buf);
+      if (more) store(blk + 1, buf ^ 1);
+    }
+  }
+  l = sum_xor32(l);
+
+  // ---- waves along the keys: folded into the first ----------------------------------------
+  if constexpr (WK > 1) {
+    float* so = reinterpret_cast<float*>(s_kv);
+    constexpr int kStride = 64 * (16 * ND + 2);   // floats of a wave's part, lane-major
+    lds_barrier();
+    if (wk > 0) {
+      float* dst = so + ((wk - 1) * WR + wr) * kStride + lane;
+      dst[0] = m;
+      dst[64] = l;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dst[64 * (2 + 16 * d + i)] = o[d][i];
+    }
+    lds_barrier();
+    if (wk > 0) return;
+#pragma unroll
+    for (int w = 0; w < WK - 1; ++w) {
+      const float* src = so + (w * WR + wr) * kStride + lane;
+      const float m2 = src[0], l2 = src[64];
+      const float m_new = fmaxf(m, m2), m_use = m_new == kNegInfF ? 0.f : m_new;
+      const float f1 = __builtin_amdgcn_exp2f(m - m_use), f2 = __builtin_amdgcn_exp2f(m2 - m_use);
+      m = m_new;
+      l = l * f1 + l2 * f2;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * f1 + src[64 * (2 + 16 * d + i)] * f2;
+    }
+  }
+  if (!real) return;
+
+  // ---- the result, or this split's part of it ----------------------------------------------
+  if (a.n_split == 1) {
+    const float v_scale = KV8 && a.v_scale ? a.v_scale[g] : 1.f;
+    const float inv = l > 0.f ? 1.f / l : 0.f;   // a row that sees no key: zeros
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        uint32_t w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const bf16x2 p = {(__bf16)(o[d][4 * i4 + 2 * k] * inv * v_scale),
+                            (__bf16)(o[d][4 * i4 + 2 * k + 1] * inv * v_scale)};
+          w[k] = __builtin_bit_cast(uint32_t, p);
+        }
+        *reinterpret_cast<u32x2*>(a.out + out_row * D + 32 * d + 8 * i4 + 4 * h) = u32x2{w[0], w[1]};
+      }
+  } else {
+    const size_t part = (size_t)split * a.runs.n_rows * Hq + out_row;
+    if (h == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, l);
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4)
+        *reinterpret_cast<f32x4*>(a.part_o + part * D + 32 * d + 8 * i4 + 4 * h) =
+            f32x4{o[d][4 * i4], o[d][4 * i4 + 1], o[d][4 * i4 + 2], o[d][4 * i4 + 3]};
+  }
+}
+
+// Folds the splits' parts: D/4 lanes a (row, query head), four outputs each, splits in order.
+template <int D>
+__global__ __launch_bounds__(256) void extend_join_kernel(const ExtendArgs a, bool kv8) {
+  constexpr int L = D / 4;
+  const int64_t item = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  const int e = 4 * (threadIdx.x % L);
+  const int Hq = a.n_q_heads;
+  const int first = a.runs.row_offsets ? run_offset(a.runs, 0) : 0;
+  const int end = a.runs.row_offsets ? run_offset(a.runs, a.runs.batch) : a.runs.n_rows;
+  const int row = (int)(item / Hq), head = (int)(item - (int64_t)row * Hq);
+  if (row < first || row >= end) return;
+  const size_t stride = (size_t)a.runs.n_rows * Hq;
+  float m = kNegInfF, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.n_split; ++s) {
+    const size_t part = s * stride + (size_t)item;
+    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * part);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e);
+    const float m_new = fmaxf(m, ml.x), m_use = m_new == kNegInfF ? 0.f : m_new;
+    const float f1 = __builtin_amdgcn_exp2f(m - m_use), f2 = __builtin_amdgcn_exp2f(ml.x - m_use);
+    m = m_new;
+    l = l * f1 + ml.y * f2;
+    o = o * f1 + x * f2;
+  }
+  const float v_scale = kv8 && a.v_scale ? a.v_scale[head / (Hq / a.n_kv_heads)] : 1.f;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const bf16x2 p = {(__bf16)(o[2 * k] * inv * v_scale), (__bf16)(o[2 * k + 1] * inv * v_scale)};
+    w[k] = __builtin_bit_cast(uint32_t, p);
+  }
+  *reinterpret_cast<u32x2*>(a.out + ((size_t)row * Hq + head) * D + e) = u32x2{w[0], w[1]};
+}
+
+template <int D, bool KV8>
+hipError_t launch_d(const ExtendPlan& p, const ExtendArgs& a, hipStream_t stream) {
+  const dim3 grid(a.n_kv_heads, p.tiles, p.n_split);
+  if (p.rows == 32) hipLaunchKernelGGL((extend_kernel<D, 1, 4, 1, KV8>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((extend_kernel<D, 8, 1, 2, KV8>), grid, dim3(512), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.n_split == 1) return e;
+  const int64_t items = (int64_t)a.runs.n_rows * a.n_q_heads;
+  const int per = 256 / (D / 4);
+  hipLaunchKernelGGL(extend_join_kernel<D>, dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, stream, a, KV8);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_extend(const ExtendPlan& p, int head_dim, bool kv8, const ExtendArgs& a, hipStream_t stream) {
+  if (head_dim == 128) return kv8 ? launch_d<128, true>(p, a, stream) : launch_d<128, false>(p, a, stream);
+  return kv8 ? launch_d<64, true>(p, a, stream) : launch_d<64, false>(p, a, stream);
+}
+
+}  // namespace delta

@@ -64,7 +64,7 @@ def queries(rows, hq, d, seed):
     return torch.randn((rows, hq, d), generator=g).to(torch.bfloat16)
 
 
-def attend(q, k, v, scale):
+def attend(q, k, v, scale, p_round=0.0):
     """float64 output [hq, d] of one row's queries over k, v [n, hkv, d], and how far a device
     result may be off in each output.
 
@@ -73,7 +73,8 @@ def attend(q, k, v, scale):
     factor exp(+-e) and another 2^-22 for exp2 and the rescalings; sums over n terms by n 2^-24; a
     split into bf16 terms of probabilities loses nothing.  Weighted by the softmax, numerator and
     denominator together are off by at most 2 (e + 2^-22 + n 2^-24) max|v|.  One rounding to bf16
-    adds 2^-8 of the result."""
+    adds 2^-8 of the result.  p_round: probabilities are rounded by at most that part of each
+    before they meet the values, which adds p_round sum p |v|."""
     hq, hkv = q.shape[0], k.shape[1]
     G = hq // hkv
     out = torch.zeros((hq, q.shape[1]), dtype=torch.float64)
@@ -87,7 +88,8 @@ def attend(q, k, v, scale):
         s = qd[rows] @ k[:, h].t().contiguous() * scale
         e = (qd[rows].abs() @ k[:, h].abs().t().contiguous() * scale).max() * (q.shape[1] + 4) * 2.0 ** -24
         out[rows] = torch.softmax(s, -1) @ v[:, h].contiguous()
-        tol[rows] = 2 * (e + 2.0 ** -22 + n * 2.0 ** -24) * v[:, h].abs().max() + out[rows].abs() * 2.0 ** -8
+        tol[rows] = p_round * (torch.softmax(s, -1) @ v[:, h].abs().contiguous())
+        tol[rows] += 2 * (e + 2.0 ** -22 + n * 2.0 ** -24) * v[:, h].abs().max() + out[rows].abs() * 2.0 ** -8
     return out, tol
 
 

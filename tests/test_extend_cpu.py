@@ -1,0 +1,77 @@
+"""Host checks of include/delta_extend.h: exports, argument refusals and workspace sizes (no GPU)."""
+import ctypes
+import os
+import re
+
+import pytest
+
+from paper_2510_09883_amd import delta as D
+from paper_2510_09883_amd import extend as E
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "delta_extend.h")
+FAKE = ctypes.c_void_p(0x1000)
+
+
+def shape(**kw):
+    s = dict(batch=4, n_q_heads=8, n_kv_heads=2, head_dim=128, max_pages_per_seq=64, max_seq_len=1024)
+    s.update(kw)
+    return D.make_shape(**s)
+
+
+def test_library_exports_the_header():
+    names = sorted(set(re.findall(r"^int (delta_\w+)\s*\(", open(HEADER).read(), re.M)))
+    assert names == sorted(E.EXPORTED)
+    lib = ctypes.CDLL(D.LIB_PATH)
+    assert all(hasattr(lib, n) for n in names)
+
+
+def append(s=None, kv=None, rope=None, n_rows=4, offsets=FAKE, q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256,
+           q_out=FAKE):
+    kv = kv or D.delta_kv_t(0x1000, 0x1000, 0x1000, 0x1000, 0)
+    return D._lib.delta_rope_append(ctypes.byref(s or shape()), ctypes.byref(kv), ctypes.byref(rope) if rope else None,
+                                    n_rows, offsets, q, qs, k, ks, v, vs, q_out, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(s=shape(head_dim=96)), -2), (dict(s=shape(n_q_heads=7)), -1), (dict(n_rows=-1), -1),
+    (dict(offsets=None, n_rows=5), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(q=None), -1),
+    (dict(q_out=None), -1), (dict(qs=1023), -1), (dict(qs=1016), -1), (dict(ks=255), -1), (dict(ks=260), -1),
+    (dict(vs=0), -1), (dict(k=ctypes.c_void_p(0x1008)), -1), (dict(q_out=ctypes.c_void_p(0x1002)), -1),
+    (dict(rope=E.delta_rope_t(None, None, 128, 0)), -1), (dict(rope=E.delta_rope_t(0x1000, None, 0, 0)), -1),
+    (dict(rope=E.delta_rope_t(0x1000, None, 24, 0)), -1), (dict(rope=E.delta_rope_t(0x1000, None, 144, 0)), -1),
+    (dict(rope=E.delta_rope_t(0x1000, None, 64, 2)), -1), (dict(n_rows=1 << 26), -2),
+    (dict(kv=D.delta_kv_t(0x1008, 0x1000, 0x1000, 0x1000, 0)), -1),
+    (dict(kv=D.delta_kv_t(0x1000, 0x1000, None, 0x1000, 0)), -1),
+    (dict(kv=D.delta_kv_t(0x1000, 0x1000, 0x1000, 0x1000, 0, 3)), -1),
+    (dict(n_rows=0, k=None, v=None, q=None, q_out=None), 0),
+])
+def test_append_arguments(kw, rc):
+    assert append(**kw) == rc
+
+
+def extend(s=None, n_rows=4, max_new=1, offsets=FAKE, q=FAKE, out=FAKE, ws=FAKE, ws_bytes=1 << 40):
+    kv = D.delta_kv_t(0x1000, 0x1000, 0x1000, 0x1000, 0)
+    return D._lib.delta_extend_attn(ctypes.byref(s or shape()), ctypes.byref(kv), n_rows, max_new, offsets, q, out,
+                                    ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(s=shape(page_size=32)), -2), (dict(n_rows=-1), -1), (dict(max_new=-1), -1), (dict(max_new=5), -1),
+    (dict(offsets=None, n_rows=3), -1), (dict(offsets=None, max_new=0), -1), (dict(q=None), -1), (dict(out=None), -1),
+    (dict(ws=None), -1), (dict(ws_bytes=8), -3), (dict(ws=ctypes.c_void_p(0x1010)), -1),
+    (dict(q=ctypes.c_void_p(0x1004)), -1), (dict(n_rows=1 << 26, max_new=4), -2),
+    (dict(n_rows=0, max_new=0), 0), (dict(max_new=0), 0),
+])
+def test_extend_arguments(kw, rc):
+    assert extend(**kw) == rc
+
+
+def test_workspace_covers_the_splits():
+    """Few rows of a long cache keep parts of their outputs; a large prompt needs none."""
+    long = shape(batch=1, max_pages_per_seq=8192, max_seq_len=131072)
+    assert D.delta_workspace_bytes(long) > 0
+    few, many = E.delta_extend_workspace_bytes(long, 1, 1), E.delta_extend_workspace_bytes(shape(), 65536, 32768)
+    assert few >= 2 * 8 * 130 * 4 and many == 256
+    assert few % 256 == 0
+    with pytest.raises(D.DeltaError):
+        E.delta_extend_workspace_bytes(shape(n_kv_heads=1, n_q_heads=16), 1, 1)
