@@ -73,7 +73,7 @@ int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int
  *            undefined)
  *   ws:      at least delta_extend_workspace_bytes() bytes, 256-byte aligned, of any content;
  *            it keeps nothing between calls.  Calls that share one must not run concurrently.
- * seq_lens[b] may be 0 (with an empty run) and is cut to max_pages_per_seq * page_size.  Keys and
+ * seq_lens[b] may be 0 (with an empty run) and is cut to max_seq_len.  Keys and
  * values of a sequence's tokens are finite; whatever else a page holds is not looked at.
  * bf16 queries, fp32 scores, softmax and sums, one bf16 rounding of the result; where a kernel
  * works on whole tiles of rows (see max_new) the probabilities are rounded to bf16 before they

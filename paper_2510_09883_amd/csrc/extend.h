@@ -47,9 +47,12 @@ struct ExtendArgs {
   uint16_t* out;
   float* part_o;             // [n_split, n_rows, Hq, D] un-normalised outputs of a split
   float* part_ml;            // [n_split, n_rows, Hq, 2] its (max, sum), log2 domain
+  int32_t* part_n;           // [n_rows, Hq] pieces of a row's keys; 0: one, whose output is written
   int64_t page_stride;
   int32_t n_q_heads, n_kv_heads;
+  int32_t max_seq_len;       // host bound of seq_lens[b] (longer ones are cut to it)
   int32_t n_split;
+  int32_t split_keys;        // keys of a piece, a multiple of every kernel's block
   float scale_log2;
   int64_t n_pages;
   uint32_t* status;          // debug status word
@@ -61,6 +64,7 @@ struct ExtendPlan {
   int rows = 0;
   int tiles = 0;
   int n_split = 1;
+  int split_keys = 0;
 };
 
 ExtendPlan plan_extend(const delta_shape_t* s, int n_rows, int max_new);

@@ -1,5 +1,7 @@
 // C ABI of the prompt side (include/delta_extend.h): argument checks, the cut of a call into tiles
 // and splits, the workspace layout, and the launches.
+#include <math.h>
+
 #include <algorithm>
 
 #include "api_common.h"
@@ -7,19 +9,45 @@
 
 namespace delta {
 
-// Tiles of 32 rows while a run fits one, of 256 otherwise; splits along the cache while the tiles
-// alone leave CUs idle.  From host-side bounds alone.
+// Which kernel, and into how many pieces the keys are cut.  The host knows no run but the longest, so
+// it takes the rows for runs of that length and single tokens.
+//
+// A workgroup of the many-row kernel takes 64 keys in 2.2 us when its 256 rows are full (a tile of a
+// single token about a quarter), one of the few-row kernel 128 keys in 1.2 us while it has a CU to
+// itself.  Keys are cut until the workgroups fill the 256 CUs (more pieces only add partial outputs
+// and their join, fewer leave CUs idle), and the kernel is the one whose last CU is done first; four
+// units of 1.2 us are what the many-row kernel's start and its LDS exchange cost more.
+// Measured on MI355X, us, few- and many-row kernel with this number of pieces, 32/8 heads, one
+// sequence: prompts of 128 tokens 6.9 and 12.2, 512 13.4 and 24, 1024 33 and 36, 2048 85 and 73, 4096
+// 303 and 168; 256 tokens behind a prefix of 7936 93 and 55; eight prompts of 256 35 and 20; eight
+// times 16 tokens at 4096 37 and 36.
 ExtendPlan plan_extend(const delta_shape_t* s, int n_rows, int max_new) {
-  ExtendPlan p;
+  constexpr int kCus = 256, kMostSplits = 32, kFewestKeys = 256, kStart = 4;
   const int G = s->n_q_heads / s->n_kv_heads;
-  p.rows = (int64_t)max_new * G <= 32 ? 32 : 256;
-  // every run ends in a partial tile: at most one more tile per run than whole ones
+  const double keys = s->max_seq_len;
+  const int spare = std::max(0, n_rows - s->batch);   // rows beyond one per sequence
+  const double runs = max_new > 1 ? std::min<double>(s->batch, std::max(1.0, round((double)spare / (max_new - 1)))) : 0;
+  struct Cut {
+    double cost;
+    int splits;
+  };
+  auto cut = [&](int rows, double light, double keys_per_unit) {
+    const double tiles = runs * ceil((double)max_new * G / rows) + light * (s->batch - runs);
+    const double wgs = std::max(1.0, tiles * s->n_kv_heads);
+    const int splits = (int)std::max(1.0, std::min({kCus / wgs, (double)kMostSplits, keys / kFewestKeys}));
+    return Cut{keys / keys_per_unit / splits * std::max(1.0, wgs * splits / kCus), splits};
+  };
+  const Cut few = cut(32, 1.0, 128), many = cut(256, 0.25, 32);
+  const bool is_few = (int64_t)max_new * G <= 32 || few.cost <= many.cost + kStart;
+  ExtendPlan p;
+  p.rows = is_few ? 32 : 256;
+  // the grid: every run ends in a partial tile, so at most one tile per run more than whole ones
   const int64_t by_run = (int64_t)s->batch * (((int64_t)max_new * G + p.rows - 1) / p.rows);
   const int64_t by_row = (int64_t)n_rows * G / p.rows + std::min(s->batch, n_rows);
   p.tiles = (int)std::min(by_run, by_row);
-  const int64_t wgs = std::max<int64_t>(1, (int64_t)p.tiles * s->n_kv_heads);
-  const int64_t want = (256 + wgs - 1) / wgs, most = std::max(1, ceil_div(s->max_seq_len, 512));
-  p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 32}));
+  const int n = is_few ? few.splits : many.splits;
+  p.split_keys = ceil_div(ceil_div(s->max_seq_len, n), kFewestKeys) * kFewestKeys;
+  p.n_split = ceil_div(s->max_seq_len, p.split_keys);
   return p;
 }
 
@@ -44,7 +72,7 @@ Runs runs_of(const delta_shape_t* s, const delta_kv_t* kv, int32_t n_rows, const
 
 struct ExtendLayout {
   ExtendPlan plan;
-  size_t status = 0, part_ml = 0, part_o = 0, total = 0;
+  size_t status = 0, part_ml = 0, part_n = 0, part_o = 0, total = 0;
 };
 
 int extend_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, ExtendLayout* L) {
@@ -59,6 +87,7 @@ int extend_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, Exten
   if (L->plan.n_split > 1) {
     const size_t parts = (size_t)L->plan.n_split * n_rows * s->n_q_heads;
     L->part_ml = off; off = align_up(off + sizeof(float) * 2 * parts);
+    L->part_n = off;  off = align_up(off + sizeof(int32_t) * (size_t)n_rows * s->n_q_heads);
     L->part_o = off;  off = align_up(off + sizeof(float) * s->head_dim * parts);
   }
   L->total = off;
@@ -155,10 +184,13 @@ int delta_extend_attn(const delta_shape_t* shape, const delta_kv_t* kv, int32_t 
   a.out = static_cast<uint16_t*>(out);
   a.part_ml = reinterpret_cast<float*>(w + L.part_ml);
   a.part_o = reinterpret_cast<float*>(w + L.part_o);
+  a.part_n = reinterpret_cast<int32_t*>(w + L.part_n);
   a.page_stride = (int64_t)shape->n_kv_heads * 16 * shape->head_dim;
   a.n_q_heads = shape->n_q_heads;
   a.n_kv_heads = shape->n_kv_heads;
+  a.max_seq_len = shape->max_seq_len;
   a.n_split = L.plan.n_split;
+  a.split_keys = L.plan.split_keys;
   a.scale_log2 = scale_log2(shape);
   a.n_pages = kv->n_pages;
   a.status = reinterpret_cast<uint32_t*>(w + L.status);

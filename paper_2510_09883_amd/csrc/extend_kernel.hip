@@ -25,7 +25,7 @@
 // LDS layouts: K rows with their 16-byte pieces permuted by the row (16 lanes reading one piece of
 // 16 rows touch all banks), V rows with their 64-byte pieces permuted by the row (the four rows of
 // a transposing read do).
-#include <type_traits>
+#include <algorithm>
 
 #include "attn_tile.h"
 #include "debug_check.h"
@@ -49,8 +49,33 @@ __device__ __forceinline__ int v_at(int r, int e) {
   return r * D + (e ^ (D == 128 ? (r & 3) << 5 : ((r >> 1) & 1) << 5));
 }
 
+// Four outputs times a factor, as bf16.
+__device__ __forceinline__ u32x2 pack_outputs(const f32x4& x, float f) {
+  u32x2 w;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const bf16x2 p = {(__bf16)(x[2 * k] * f), (__bf16)(x[2 * k + 1] * f)};
+    w[k] = __builtin_bit_cast(uint32_t, p);
+  }
+  return w;
+}
+
+// What a workgroup knows of its tile.
+struct TileOf {
+  int b;         // the sequence
+  int begin;     // first row of its run
+  int n_rows;    // (token, query head) rows of its run
+  int n_new;     // tokens of its run
+  int first;     // first of the rows that the tile takes
+  int s_b;       // tokens of the sequence
+};
+
+// LDS of a body, in bytes: K and V of the blocks, later the outputs of the waves along the keys.
+template <int D, int WR, int WK, int KT>
+constexpr int kBodyLds = std::max(2 * (WR == 1 ? 1 : 2) * 32 * KT * WK * D * 2, WK > 1 ? WK * 64 * D / 2 * 4 : 0);
+
 template <int D, int WR, int WK, int KT, bool KV8>
-__global__ __launch_bounds__(64 * WR * WK, 1) void extend_kernel(const ExtendArgs a) {
+__device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t, uint16_t* s_kv, float2* s_ml) {
   constexpr int NW = WR * WK, T = 64 * NW;
   constexpr int BM = 32 * WR;           // rows of a tile
   constexpr int BK = 32 * KT;           // keys a wave takes of a block
@@ -63,59 +88,35 @@ __global__ __launch_bounds__(64 * WR * WK, 1) void extend_kernel(const ExtendArg
   constexpr int NL = (kPieces + T - 1) / T;   // loads per thread and block (the last waves may have none)
   constexpr int RPW = 64 / CPR;         // rows of a wave-wide load
   static_assert(kPieces % 64 == 0 && 16 % RPW == 0, "whole loads, each inside one page");
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave % WR, wk = wave / WR;
   const int n = lane & 31, h = lane >> 5;
   const int g = blockIdx.x, split = blockIdx.z;
   const int Hq = a.n_q_heads, G = Hq / a.n_kv_heads;
 
+  // Waves that share no rows share no keys either: each brings its own keys to its own LDS, without
+  // barriers, and needs one buffer of it.
+  constexpr bool kOwnKeys = WR == 1;
+  constexpr int kBuffers = kOwnKeys ? 1 : 2;
   constexpr int kBlock = BN * D;        // elements of a K or V block
-  constexpr int kMerge = WK > 1 ? (WK - 1) * WR * 64 * (16 * ND + 2) * 2 : 0;   // (in 16-bit units)
-  constexpr int kLds = 4 * kBlock > kMerge ? 4 * kBlock : kMerge;
-  __shared__ __attribute__((aligned(256))) uint16_t s_kv[kLds];   // K, V of two blocks; then the merge
-
-  // ---- the tile: which sequence, which of its rows ----------------------------------------
-  int tile = blockIdx.y, b = 0, begin = 0, n_new = 0;
-  bool found = false;
-  for (int c = 0; c < a.runs.batch && !found; c += 64) {
-    int lo = 0, len = 0;
-    if (c + lane < a.runs.batch) {
-      lo = run_offset(a.runs, c + lane);
-      len = max(0, run_offset(a.runs, c + lane + 1) - lo);
-    }
-    const int tiles = (int)(((int64_t)len * G + BM - 1) / BM);
-    const int incl = wave_incl_scan(tiles);
-    const uint64_t past = __ballot(incl > tile);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      b = c + l;
-      begin = __builtin_amdgcn_readlane(lo, l);
-      n_new = __builtin_amdgcn_readlane(len, l);
-      const int mine = __builtin_amdgcn_readlane(tiles, l);
-      tile -= __builtin_amdgcn_readlane(incl, l) - mine;
-      tile = mine - 1 - tile;   // the last rows see most keys: they start first
-      found = true;
-    } else {
-      tile -= __builtin_amdgcn_readlane(incl, 63);
-    }
-  }
-  if (!found) return;
-  const int s_b = max(0, min(a.runs.seq_lens[b], 16 * a.runs.max_pages));
-  const int n_tile_rows = n_new * G;    // (n_rows * Hq < 2^31)
+  const int b = t.b, n_new = t.n_new, s_b = t.s_b, n_tile_rows = t.n_rows, begin = t.begin;
   // this lane's row: token j of the run, query head g * G + head
-  const int r0 = tile * BM + 32 * wr;
+  const int r0 = t.first + 32 * wr;
   const int r = min(r0 + n, n_tile_rows - 1);
   const bool real = r0 + n < n_tile_rows;
+  const bool active = r0 < n_tile_rows;                               // some row of the wave is
   const int j = r / G, head = g * G + (r - j * G);
   const size_t out_row = (size_t)(begin + j) * Hq + head;
   const int lim = max(0, s_b - n_new + j + 1);                        // keys the row sees
   auto lim_of = [&](int row) { return max(0, s_b - n_new + min(row, n_tile_rows - 1) / G + 1); };
   const int lim_lo = lim_of(r0), lim_hi = lim_of(r0 + 31);            // of the wave's rows
-  const int lim_tile = lim_of(tile * BM + BM - 1);
 
-  const int n_blocks = (lim_tile + BN - 1) / BN;
-  const int per_split = (n_blocks + a.n_split - 1) / a.n_split;
+  const int n_blocks = (lim_of(t.first + BM - 1) + BN - 1) / BN;
+  // pieces of one length whatever the sequence's: a short sequence has fewer
+  const int per_split = a.split_keys / BN;
+  const int n_valid = max(1, (n_blocks + per_split - 1) / per_split);
+  if (split >= n_valid) return;
   const int blk0 = split * per_split, blk1 = min(n_blocks, blk0 + per_split);
 
   const float scale = KV8 && a.k_scale ? a.scale_log2 * a.k_scale[g] : a.scale_log2;
@@ -123,6 +124,10 @@ __global__ __launch_bounds__(64 * WR * WK, 1) void extend_kernel(const ExtendArg
 #pragma unroll
   for (int ks = 0; ks < NK; ++ks)
     q[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(a.q + out_row * D + 16 * ks + 8 * h));
+  // they are waited for here: a wait for their first use, inside the loop, would also wait for the
+  // loads of the next block in every round
+#pragma unroll
+  for (int ks = 0; ks < NK; ++ks) asm volatile("" : "+v"(q[ks]));
 
   float m = kNegInfF, l = 0.f;
   f32x16 o[ND];
@@ -139,17 +144,24 @@ __global__ __launch_bounds__(64 * WR * WK, 1) void extend_kernel(const ExtendArg
     page_base = base;
   };
   u32x4 kr[NL], vr[NL];
+  // the wave's first row of load i, in the block
+  auto row_of = [&](int i) { return kOwnKeys ? wk * BK + i * RPW : (i * NW + wave) * RPW; };
   auto load = [&](int blk) {
     const int first = blk * BN / 16;
     if (first + BN / 16 > page_base + 64) list_pages(first);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int row = (i * NW + wave) * RPW;   // the wave's first row of this load, in the block
+      const int row = row_of(i);
       if (kPieces % T && row >= BN) break;
       const int page = __builtin_amdgcn_readlane(pages, first + row / 16 - page_base);
       const size_t at = ((size_t)page * a.page_stride + (size_t)(g * 16 + row % 16) * D) * EB + 16 * lane;
-      kr[i] = *reinterpret_cast<const u32x4*>(a.k_cache + at);
-      vr[i] = *reinterpret_cast<const u32x4*>(a.v_cache + at);
+      if constexpr (kOwnKeys) {
+        kr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.k_cache + at));
+        vr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.v_cache + at));
+      } else {
+        kr[i] = *reinterpret_cast<const u32x4*>(a.k_cache + at);
+        vr[i] = *reinterpret_cast<const u32x4*>(a.v_cache + at);
+      }
     }
   };
   auto store = [&](int blk, int buf) {
@@ -157,7 +169,7 @@ __global__ __launch_bounds__(64 * WR * WK, 1) void extend_kernel(const ExtendArg
     uint16_t* sv = sk + kBlock;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int row = (i * NW + wave) * RPW + lane / CPR, c = lane % CPR;
+      const int row = row_of(i) + lane / CPR, c = lane % CPR;
       if (kPieces % T && row >= BN) break;
       u32x4 v = vr[i];
       // rows past the sequence: 0 times what they hold (NaN) would spoil the sums
@@ -185,7 +197,7 @@ __global__ __launch_bounds__(64 * WR * WK, 1) void extend_kernel(const ExtendArg
 
   auto attend = [&](int blk, int buf) {
     const int key0 = blk * BN + wk * BK;   // the wave's first key
-    if (key0 >= lim_hi) return;
+    if ((WR > 1 && !active) || key0 >= lim_hi) return;
     const uint16_t* sk = s_kv + buf * 2 * kBlock + wk * BK * D;
     const uint16_t* sv = s_kv + buf * 2 * kBlock + kBlock + wk * BK * D;
     f32x16 s[KT];
@@ -268,75 +280,127 @@ __global__ __launch_bounds__(64 * WR * WK, 1) void extend_kernel(const ExtendArg
     load(blk0);
     store(blk0, 0);
     for (int blk = blk0; blk < blk1; ++blk) {
-      const int buf = (blk - blk0) & 1;
+      const int buf = kBuffers == 2 ? (blk - blk0) & 1 : 0;
       const bool more = blk + 1 < blk1;
       if (more) load(blk + 1);
-      lds_barrier();   // the block is in LDS, and nobody reads the other buffer any more
+      // the block is in LDS, and nobody reads the other buffer any more
+      if (kOwnKeys) wave_lds_sync();
+      else lds_barrier();
       attend(blk, buf);
-      if (more) store(blk + 1, buf ^ 1);
+      if (kOwnKeys) wave_lds_sync();
+      if (more) store(blk + 1, kBuffers == 2 ? buf ^ 1 : 0);
     }
   }
   l = sum_xor32(l);
 
-  // ---- waves along the keys: folded into the first ----------------------------------------
-  if constexpr (WK > 1) {
-    float* so = reinterpret_cast<float*>(s_kv);
-    constexpr int kStride = 64 * (16 * ND + 2);   // floats of a wave's part, lane-major
-    lds_barrier();
-    if (wk > 0) {
-      float* dst = so + ((wk - 1) * WR + wr) * kStride + lane;
-      dst[0] = m;
-      dst[64] = l;
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) dst[64 * (2 + 16 * d + i)] = o[d][i];
-    }
-    lds_barrier();
-    if (wk > 0) return;
-#pragma unroll
-    for (int w = 0; w < WK - 1; ++w) {
-      const float* src = so + (w * WR + wr) * kStride + lane;
-      const float m2 = src[0], l2 = src[64];
-      const float m_new = fmaxf(m, m2), m_use = m_new == kNegInfF ? 0.f : m_new;
-      const float f1 = __builtin_amdgcn_exp2f(m - m_use), f2 = __builtin_amdgcn_exp2f(m2 - m_use);
-      m = m_new;
-      l = l * f1 + l2 * f2;
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * f1 + src[64 * (2 + 16 * d + i)] * f2;
-    }
-  }
-  if (!real) return;
+  // ---- the result, or this split's part of it: outputs e .. e + 3 of the lane's row ----------
+  const float v_scale = KV8 && a.v_scale ? a.v_scale[g] : 1.f;
+  const size_t part = (size_t)split * a.runs.n_rows * Hq + out_row;
+  auto emit = [&](const f32x4& x, float inv, int e) {
+    if (n_valid > 1) *reinterpret_cast<f32x4*>(a.part_o + part * D + e) = x;
+    else *reinterpret_cast<u32x2*>(a.out + out_row * D + e) = pack_outputs(x, inv * v_scale);
+  };
+  auto emit_sums = [&]() {
+    if (a.n_split > 1 && split == 0) a.part_n[out_row] = n_valid > 1 ? n_valid : 0;
+    if (n_valid > 1) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, l);
+  };
 
-  // ---- the result, or this split's part of it ----------------------------------------------
-  if (a.n_split == 1) {
-    const float v_scale = KV8 && a.v_scale ? a.v_scale[g] : 1.f;
+  if constexpr (WK == 1) {
+    if (!real) return;
+    if (h == 0) emit_sums();
     const float inv = l > 0.f ? 1.f / l : 0.f;   // a row that sees no key: zeros
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        uint32_t w[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const bf16x2 p = {(__bf16)(o[d][4 * i4 + 2 * k] * inv * v_scale),
-                            (__bf16)(o[d][4 * i4 + 2 * k + 1] * inv * v_scale)};
-          w[k] = __builtin_bit_cast(uint32_t, p);
-        }
-        *reinterpret_cast<u32x2*>(a.out + out_row * D + 32 * d + 8 * i4 + 4 * h) = u32x2{w[0], w[1]};
-      }
+      for (int i = 0; i < 4; ++i)
+        emit(f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]}, inv, 32 * d + 8 * i + 4 * h);
   } else {
-    const size_t part = (size_t)split * a.runs.n_rows * Hq + out_row;
-    if (h == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, l);
+    // Waves along the keys are joined through LDS, in their order: each takes a share of the
+    // outputs (of every row) and reads it from all.
+    static_assert(WR == 1 && 4 * ND % WK == 0, "whole shares");
+    constexpr int kShare = 4 * ND / WK;           // groups of four outputs
+    f32x4* so = reinterpret_cast<f32x4*>(s_kv);   // [WK][4 * ND][64]
+    lds_barrier();
+    s_ml[wk * 64 + lane] = make_float2(m, l);
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+    for (int f = 0; f < 4 * ND; ++f)
+      so[(wk * 4 * ND + f) * 64 + lane] =
+          f32x4{o[f / 4][4 * (f % 4)], o[f / 4][4 * (f % 4) + 1], o[f / 4][4 * (f % 4) + 2], o[f / 4][4 * (f % 4) + 3]};
+    lds_barrier();
+    if (!real) return;
+    float f[WK];
+    m = kNegInfF;
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4)
-        *reinterpret_cast<f32x4*>(a.part_o + part * D + 32 * d + 8 * i4 + 4 * h) =
-            f32x4{o[d][4 * i4], o[d][4 * i4 + 1], o[d][4 * i4 + 2], o[d][4 * i4 + 3]};
+    for (int w = 0; w < WK; ++w) m = fmaxf(m, s_ml[w * 64 + lane].x);
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < WK; ++w) {
+      const float2 ml = s_ml[w * 64 + lane];
+      f[w] = __builtin_amdgcn_exp2f(ml.x - (m == kNegInfF ? 0.f : m));
+      l += f[w] * ml.y;
+    }
+    if (wk == 0 && h == 0) emit_sums();
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int c = 0; c < kShare; ++c) {
+      const int at = wk * kShare + c;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < WK; ++w) x += f[w] * so[(w * 4 * ND + at) * 64 + lane];
+      emit(x, inv, 8 * at + 4 * h);
+    }
   }
+}
+
+// The tile of this workgroup: which sequence, which of its rows; false: there is none.
+template <int ROWS>
+__device__ __forceinline__ bool find_tile(const ExtendArgs& a, TileOf& t) {
+  const int lane = threadIdx.x & 63, G = a.n_q_heads / a.n_kv_heads;
+  int tile = blockIdx.y;
+  for (int c = 0; c < a.runs.batch; c += 64) {
+    int lo = 0, len = 0;
+    if (c + lane < a.runs.batch) {
+      lo = run_offset(a.runs, c + lane);
+      len = max(0, run_offset(a.runs, c + lane + 1) - lo);
+    }
+    const int tiles = (int)(((int64_t)len * G + ROWS - 1) / ROWS);
+    const int incl = wave_incl_scan(tiles);
+    const uint64_t past = __ballot(incl > tile);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      t.b = c + l;
+      t.begin = __builtin_amdgcn_readlane(lo, l);
+      t.n_new = __builtin_amdgcn_readlane(len, l);
+      t.n_rows = t.n_new * G;   // (n_rows * Hq < 2^31)
+      // the last rows see most keys: they start first
+      t.first = (__builtin_amdgcn_readlane(incl, l) - 1 - tile) * ROWS;
+      t.s_b = max(0, min(a.runs.seq_lens[t.b], a.max_seq_len));
+      return true;
+    }
+    tile -= __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+// Tiles of 32 rows, four waves along the keys.
+template <int D, bool KV8>
+__global__ __launch_bounds__(256, 2) void extend_few_kernel(const ExtendArgs a) {
+  __shared__ __attribute__((aligned(256))) uint16_t s_kv[kBodyLds<D, 1, 4, 1> / 2];
+  __shared__ float2 s_ml[4 * 64];
+  TileOf t;
+  if (find_tile<32>(a, t)) extend_body<D, 1, 4, 1, KV8>(a, t, s_kv, s_ml);
+}
+
+// Tiles of 256 rows, eight waves along them; a tile that has no more than 32 (a single token beside
+// prompts) is taken by eight waves along its keys instead of by one.
+template <int D, bool KV8>
+__global__ __launch_bounds__(512, 1) void extend_many_kernel(const ExtendArgs a) {
+  __shared__ __attribute__((aligned(256))) uint16_t s_kv[std::max(kBodyLds<D, 8, 1, 2>, kBodyLds<D, 1, 8, 1>) / 2];
+  __shared__ float2 s_ml[8 * 64];
+  TileOf t;
+  if (!find_tile<256>(a, t)) return;
+  if (t.n_rows - t.first <= 32) extend_body<D, 1, 8, 1, KV8>(a, t, s_kv, s_ml);
+  else extend_body<D, 8, 1, 2, KV8>(a, t, s_kv, s_ml);
 }
 
 // Folds the splits' parts: D/4 lanes a (row, query head), four outputs each, splits in order.
@@ -351,9 +415,11 @@ __global__ __launch_bounds__(256) void extend_join_kernel(const ExtendArgs a, bo
   const int row = (int)(item / Hq), head = (int)(item - (int64_t)row * Hq);
   if (row < first || row >= end) return;
   const size_t stride = (size_t)a.runs.n_rows * Hq;
+  const int n = a.part_n[item];   // 0: written by its only piece
+  if (n == 0) return;
   float m = kNegInfF, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.n_split; ++s) {
+  for (int s = 0; s < n; ++s) {
     const size_t part = s * stride + (size_t)item;
     const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * part);
     const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e);
@@ -365,20 +431,14 @@ __global__ __launch_bounds__(256) void extend_join_kernel(const ExtendArgs a, bo
   }
   const float v_scale = kv8 && a.v_scale ? a.v_scale[head / (Hq / a.n_kv_heads)] : 1.f;
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  uint32_t w[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const bf16x2 p = {(__bf16)(o[2 * k] * inv * v_scale), (__bf16)(o[2 * k + 1] * inv * v_scale)};
-    w[k] = __builtin_bit_cast(uint32_t, p);
-  }
-  *reinterpret_cast<u32x2*>(a.out + ((size_t)row * Hq + head) * D + e) = u32x2{w[0], w[1]};
+  *reinterpret_cast<u32x2*>(a.out + (size_t)item * D + e) = pack_outputs(o, inv * v_scale);
 }
 
 template <int D, bool KV8>
 hipError_t launch_d(const ExtendPlan& p, const ExtendArgs& a, hipStream_t stream) {
   const dim3 grid(a.n_kv_heads, p.tiles, p.n_split);
-  if (p.rows == 32) hipLaunchKernelGGL((extend_kernel<D, 1, 4, 1, KV8>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((extend_kernel<D, 8, 1, 2, KV8>), grid, dim3(512), 0, stream, a);
+  if (p.rows == 32) hipLaunchKernelGGL((extend_few_kernel<D, KV8>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((extend_many_kernel<D, KV8>), grid, dim3(512), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_split == 1) return e;
   const int64_t items = (int64_t)a.runs.n_rows * a.n_q_heads;

@@ -157,6 +157,9 @@ def _check_kv(kv, shape):
     t = getattr(kv, "_tensors", None)
     if t is None:   # built by hand from raw pointers: nothing to check
         return
+    # make_kv found tensors that fit these sizes: five comparisons instead of four checks (3 us)
+    if kv._fits == (shape.n_kv_heads, shape.page_size, shape.head_dim, shape.batch, shape.max_pages_per_seq):
+        return
     k, v, pt, sl, scales = t
     cache = (None, shape.n_kv_heads, shape.page_size, shape.head_dim)
     kind = torch.float8_e4m3fn if kv.kv_type == DELTA_KV_E4M3 else torch.bfloat16
@@ -183,7 +186,8 @@ def _check_sel(shape, sel, sel_idx, sel_cnt, sel_phys=None):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    # (the stream object behind torch.cuda.current_stream() costs another 1 us)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def make_shape(batch, n_q_heads, n_kv_heads, head_dim, max_pages_per_seq, max_seq_len,
@@ -213,7 +217,20 @@ def make_kv(k_cache, v_cache, page_table, seq_lens, k_scale=None, v_scale=None) 
     kv = delta_kv_t(k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
                     k_cache.shape[0], DELTA_KV_E4M3 if e4m3 else DELTA_KV_BF16, _ptr(k_scale), _ptr(v_scale))
     kv._tensors = (k_cache, v_cache, page_table, seq_lens, scales)   # checked against the shape per call
+    kv._fits = _sizes_that_fit(*kv._tensors)
     return kv
+
+
+def _sizes_that_fit(k, v, pt, sl, scales):
+    """The (n_kv_heads, page_size, head_dim, batch, max_pages_per_seq) that a cache's tensors were
+    made for, or None if their types or shapes fit no shape (the check of a call says why)."""
+    kind = torch.float8_e4m3fn if k.dtype == torch.float8_e4m3fn else torch.bfloat16
+    if not (k.dtype == v.dtype == kind and pt.dtype == sl.dtype == torch.int32 and k.dim() == 4
+            and v.shape[1:] == k.shape[1:] and pt.dim() == 2 and tuple(sl.shape) == (pt.shape[0],)):
+        return None
+    if any(s.dtype != torch.float32 or tuple(s.shape) != (k.shape[1],) for _, s in scales):
+        return None
+    return (*k.shape[1:], *pt.shape)
 
 
 def delta_build_flags() -> int:

@@ -31,7 +31,12 @@ for _n in EXPORTED:
 
 
 def _rows(name, t, heads, d):
-    """A bf16 [rows, heads, d] GPU tensor whose rows may stand apart; its row stride."""
+    """A bf16 [rows, heads, d] GPU tensor whose rows may stand apart; its row stride.  What passes is
+    found out first, and what does not is given its message after."""
+    if type(t) is torch.Tensor and t.is_cuda and t.dtype == torch.bfloat16:
+        have, stride = t.shape, t.stride()
+        if have[1:] == (heads, d) and stride[1:] == (d, 1):
+            return stride[0] if have[0] > 1 else heads * d   # (the stride of a single row says nothing)
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
     if not t.is_cuda:
@@ -41,12 +46,9 @@ def _rows(name, t, heads, d):
     if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
         raise ValueError(f"{name}: expected shape {(None, heads, d)}, got {tuple(t.shape)}")
     row, head, elem = t.stride()
-    if t.shape[0] < 2:
-        row = max(row, heads * d)   # (the stride of a single row says nothing)
-        row += -row % 8
-    if t.numel() and ((elem != 1 and d > 1) or (head != d and heads > 1)):
+    if t.numel() and (elem != 1 or (head != d and heads > 1)):
         raise ValueError(f"{name}: the heads of a row must lie one behind the other")
-    return row
+    return heads * d if t.shape[0] < 2 else row
 
 
 def _offsets(row_offsets, batch):
@@ -57,7 +59,7 @@ def _offsets(row_offsets, batch):
 def _same_device(*tensors):
     here = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device.index != here:
+        if t is not None and t.get_device() != here:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
 
 
