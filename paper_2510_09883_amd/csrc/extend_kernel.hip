@@ -146,6 +146,7 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   u32x4 kr[NL], vr[NL];
   // the wave's first row of load i, in the block
   auto row_of = [&](int i) { return kOwnKeys ? wk * BK + i * RPW : (i * NW + wave) * RPW; };
+  const uint32_t lane16 = 16 * lane;
   auto load = [&](int blk) {
     const int first = blk * BN / 16;
     if (first + BN / 16 > page_base + 64) list_pages(first);
@@ -154,14 +155,12 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
       const int row = row_of(i);
       if (kPieces % T && row >= BN) break;
       const int page = __builtin_amdgcn_readlane(pages, first + row / 16 - page_base);
-      const size_t at = ((size_t)page * a.page_stride + (size_t)(g * 16 + row % 16) * D) * EB + 16 * lane;
-      if constexpr (kOwnKeys) {
-        kr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.k_cache + at));
-        vr[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.v_cache + at));
-      } else {
-        kr[i] = *reinterpret_cast<const u32x4*>(a.k_cache + at);
-        vr[i] = *reinterpret_cast<const u32x4*>(a.v_cache + at);
-      }
+      // (uniform: scalar arithmetic, and the lane's offset is the loads' own)
+      const size_t at = ((size_t)(uint32_t)page * (uint32_t)a.page_stride + (uint32_t)((g * 16 + row % 16) * D)) * EB;
+      const u32x4* kp = reinterpret_cast<const u32x4*>(a.k_cache + at + lane16);
+      const u32x4* vp = reinterpret_cast<const u32x4*>(a.v_cache + at + lane16);
+      kr[i] = kOwnKeys ? __builtin_nontemporal_load(kp) : *kp;
+      vr[i] = kOwnKeys ? __builtin_nontemporal_load(vp) : *vp;
     }
   };
   auto store = [&](int blk, int buf) {

@@ -9,7 +9,7 @@ import ctypes
 
 import torch
 
-from .delta import DeltaError, _check, _check_kv, _dev, _lib, _nbytes, _P, _ptr, _stream, _vp
+from .delta import DeltaError, _check, _check_kv, _dev, _lib, _nbytes, _P, _ptr, _vp
 from .delta import delta_kv_t, delta_shape_t
 
 EXPORTED = ["delta_rope_append", "delta_extend_workspace_bytes", "delta_extend_attn"]
@@ -56,11 +56,13 @@ def _offsets(row_offsets, batch):
         _dev("row_offsets", row_offsets, torch.int32, (batch + 1,))
 
 
-def _same_device(*tensors):
+def _stream_of(*tensors):
+    """The current device's current stream; every tensor has to be on that device."""
     here = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+    return torch._C._cuda_getCurrentRawStream(here)
 
 
 def delta_rope_append(shape, kv: delta_kv_t, q, k, v, q_out, inv_freq=None, row_offsets=None,
@@ -92,10 +94,10 @@ def delta_rope_append(shape, kv: delta_kv_t, q, k, v, q_out, inv_freq=None, row_
                                          1 if interleaved else 0))
     elif positions is not None:
         raise ValueError("positions: nothing is rotated without inv_freq")
-    _same_device(k, v, q, q_out, row_offsets, inv_freq, positions)
+    stream = _stream_of(k, v, q, q_out, row_offsets, inv_freq, positions)
     _check("delta_rope_append",
            _lib.delta_rope_append(ctypes.byref(shape), ctypes.byref(kv), rope, n, _ptr(row_offsets),
-                                  _ptr(q), qs, k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q_out), _stream()))
+                                  _ptr(q), qs, k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q_out), stream))
 
 
 def delta_extend_workspace_bytes(shape: delta_shape_t, n_rows: int, max_new: int) -> int:
@@ -118,10 +120,10 @@ def delta_extend_attn(shape, kv: delta_kv_t, q, out, row_offsets, max_new, ws):
     _dev("out", out, torch.bfloat16, tuple(q.shape))
     _offsets(row_offsets, shape.batch)
     _dev("ws", ws)
-    _same_device(q, out, row_offsets, ws)
+    stream = _stream_of(q, out, row_offsets, ws)
     _check("delta_extend_attn",
            _lib.delta_extend_attn(ctypes.byref(shape), ctypes.byref(kv), q.shape[0], max_new,
-                                  _ptr(row_offsets), _ptr(q), _ptr(out), _ptr(ws), _nbytes(ws), _stream()))
+                                  _ptr(row_offsets), _ptr(q), _ptr(out), _ptr(ws), _nbytes(ws), stream))
 
 
 __all__ = ["DeltaError", "delta_rope_t", "delta_rope_append", "delta_extend_workspace_bytes",
