@@ -49,12 +49,15 @@ __device__ __forceinline__ int v_at(int r, int e) {
   return r * D + (e ^ (D == 128 ? (r & 3) << 5 : ((r >> 1) & 1) << 5));
 }
 
-// Four outputs times a factor, as bf16.
-__device__ __forceinline__ u32x2 pack_outputs(const f32x4& x, float f) {
+// Four outputs, scaled and divided by the softmax sum, as bf16; a row that sees no key (l = 0) gets
+// zeros.  (Divided: a product by 1 / l has a rounding more, which moves quotients half way between
+// two bf16 values, as equal weights give.)
+__device__ __forceinline__ u32x2 pack_outputs(const f32x4& x, float scale, float l) {
   u32x2 w;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const bf16x2 p = {(__bf16)(x[2 * k] * f), (__bf16)(x[2 * k + 1] * f)};
+    const float a = x[2 * k] * scale, b = x[2 * k + 1] * scale;
+    const bf16x2 p = {(__bf16)(l > 0.f ? a / l : 0.f), (__bf16)(l > 0.f ? b / l : 0.f)};
     w[k] = __builtin_bit_cast(uint32_t, p);
   }
   return w;
@@ -295,9 +298,9 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   // ---- the result, or this split's part of it: outputs e .. e + 3 of the lane's row ----------
   const float v_scale = KV8 && a.v_scale ? a.v_scale[g] : 1.f;
   const size_t part = (size_t)split * a.runs.n_rows * Hq + out_row;
-  auto emit = [&](const f32x4& x, float inv, int e) {
+  auto emit = [&](const f32x4& x, int e) {
     if (n_valid > 1) *reinterpret_cast<f32x4*>(a.part_o + part * D + e) = x;
-    else *reinterpret_cast<u32x2*>(a.out + out_row * D + e) = pack_outputs(x, inv * v_scale);
+    else *reinterpret_cast<u32x2*>(a.out + out_row * D + e) = pack_outputs(x, v_scale, l);
   };
   auto emit_sums = [&]() {
     if (a.n_split > 1 && split == 0) a.part_n[out_row] = n_valid > 1 ? n_valid : 0;
@@ -307,12 +310,11 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   if constexpr (WK == 1) {
     if (!real) return;
     if (h == 0) emit_sums();
-    const float inv = l > 0.f ? 1.f / l : 0.f;   // a row that sees no key: zeros
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        emit(f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]}, inv, 32 * d + 8 * i + 4 * h);
+        emit(f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]}, 32 * d + 8 * i + 4 * h);
   } else {
     // Waves along the keys are joined through LDS, in their order: each takes a share of the
     // outputs (of every row) and reads it from all.
@@ -339,14 +341,13 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
       l += f[w] * ml.y;
     }
     if (wk == 0 && h == 0) emit_sums();
-    const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
     for (int c = 0; c < kShare; ++c) {
       const int at = wk * kShare + c;
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < WK; ++w) x += f[w] * so[(w * 4 * ND + at) * 64 + lane];
-      emit(x, inv, 8 * at + 4 * h);
+      emit(x, 8 * at + 4 * h);
     }
   }
 }
@@ -429,8 +430,7 @@ __global__ __launch_bounds__(256) void extend_join_kernel(const ExtendArgs a, bo
     o = o * f1 + x * f2;
   }
   const float v_scale = kv8 && a.v_scale ? a.v_scale[head / (Hq / a.n_kv_heads)] : 1.f;
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  *reinterpret_cast<u32x2*>(a.out + (size_t)item * D + e) = pack_outputs(o, inv * v_scale);
+  *reinterpret_cast<u32x2*>(a.out + (size_t)item * D + e) = pack_outputs(o, v_scale, l);
 }
 
 template <int D, bool KV8>

@@ -9,7 +9,8 @@ import ctypes
 
 import torch
 
-from .delta import DeltaError, _check, _check_kv, _dev, _lib, _nbytes, _P, _ptr, _vp
+from . import delta
+from .delta import DeltaError, _check, _check_kv, _dev, _nbytes, _P, _ptr, _vp
 from .delta import delta_kv_t, delta_shape_t
 
 EXPORTED = ["delta_rope_append", "delta_extend_workspace_bytes", "delta_extend_attn"]
@@ -21,13 +22,21 @@ class delta_rope_t(ctypes.Structure):
 
 
 _i32, _i64 = ctypes.c_int32, ctypes.c_int64
-_lib.delta_rope_append.argtypes = [_P(delta_shape_t), _P(delta_kv_t), _P(delta_rope_t), _i32, _vp,
-                                   _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
-_lib.delta_extend_workspace_bytes.argtypes = [_P(delta_shape_t), _i32, _i32, _P(ctypes.c_size_t)]
-_lib.delta_extend_attn.argtypes = [_P(delta_shape_t), _P(delta_kv_t), _i32, _i32, _vp, _vp, _vp, _vp,
-                                   ctypes.c_size_t, _vp]
-for _n in EXPORTED:
-    getattr(_lib, _n).restype = ctypes.c_int
+
+
+def _bind(lib):
+    """Declare the C signatures of include/delta_extend.h on a loaded library handle."""
+    lib.delta_rope_append.argtypes = [_P(delta_shape_t), _P(delta_kv_t), _P(delta_rope_t), _i32, _vp,
+                                      _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
+    lib.delta_extend_workspace_bytes.argtypes = [_P(delta_shape_t), _i32, _i32, _P(ctypes.c_size_t)]
+    lib.delta_extend_attn.argtypes = [_P(delta_shape_t), _P(delta_kv_t), _i32, _i32, _vp, _vp, _vp, _vp,
+                                      ctypes.c_size_t, _vp]
+    for n in EXPORTED:
+        getattr(lib, n).restype = ctypes.c_int
+    return lib
+
+
+_bind(delta._lib)   # (calls go to the library that the decode-step binding has loaded)
 
 
 def _rows(name, t, heads, d):
@@ -96,14 +105,14 @@ def delta_rope_append(shape, kv: delta_kv_t, q, k, v, q_out, inv_freq=None, row_
         raise ValueError("positions: nothing is rotated without inv_freq")
     stream = _stream_of(k, v, q, q_out, row_offsets, inv_freq, positions)
     _check("delta_rope_append",
-           _lib.delta_rope_append(ctypes.byref(shape), ctypes.byref(kv), rope, n, _ptr(row_offsets),
-                                  _ptr(q), qs, k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q_out), stream))
+           delta._lib.delta_rope_append(ctypes.byref(shape), ctypes.byref(kv), rope, n, _ptr(row_offsets),
+                                        _ptr(q), qs, k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q_out), stream))
 
 
 def delta_extend_workspace_bytes(shape: delta_shape_t, n_rows: int, max_new: int) -> int:
     n = ctypes.c_size_t(0)
     _check("delta_extend_workspace_bytes",
-           _lib.delta_extend_workspace_bytes(ctypes.byref(shape), n_rows, max_new, ctypes.byref(n)))
+           delta._lib.delta_extend_workspace_bytes(ctypes.byref(shape), n_rows, max_new, ctypes.byref(n)))
     return n.value
 
 
@@ -122,8 +131,8 @@ def delta_extend_attn(shape, kv: delta_kv_t, q, out, row_offsets, max_new, ws):
     _dev("ws", ws)
     stream = _stream_of(q, out, row_offsets, ws)
     _check("delta_extend_attn",
-           _lib.delta_extend_attn(ctypes.byref(shape), ctypes.byref(kv), q.shape[0], max_new,
-                                  _ptr(row_offsets), _ptr(q), _ptr(out), _ptr(ws), _nbytes(ws), stream))
+           delta._lib.delta_extend_attn(ctypes.byref(shape), ctypes.byref(kv), q.shape[0], max_new,
+                                        _ptr(row_offsets), _ptr(q), _ptr(out), _ptr(ws), _nbytes(ws), stream))
 
 
 __all__ = ["DeltaError", "delta_rope_t", "delta_rope_append", "delta_extend_workspace_bytes",
