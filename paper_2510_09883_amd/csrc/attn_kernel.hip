@@ -60,7 +60,9 @@ constexpr int kCoherent = 16;   // cache-policy operand of the buffer builtins: 
 constexpr int kPastEnd = 0x7ffffff0;   // a byte offset past every buffer
 // LDS floats for staging Delta-layer logits (128 KB: one Delta workgroup per CU; measured on
 // MI355X, fewer and larger chunk flushes beat two resident workgroups with half the staging).
-constexpr int kStageFloats = 32768;
+// An e4m3 cache's pairs of tiles take 16 KB more of the LDS.
+template <bool KV8>
+constexpr int kStageFloats = KV8 ? 28672 : 32768;
 
 // Page list entries of the selected-page mode: the page, and whether only the sequence's tail
 // rows (kPartialPage) or none of its rows (kEmptyPage, the sign bit) exist.
@@ -73,6 +75,7 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
   static_assert(!BAL || MODE == ROWS_DENSE, "the balanced decomposition is for dense launches");
   using Gm = Geo<D>;
   using CacheTile = std::conditional_t<KV8, Tile8<D>, Tile<D>>;
+  constexpr int SG = KV8 ? 2 : 1;   // groups that a wave folds at a time
   constexpr int R = KV8 ? Geo8<D>::R : Gm::R;
   constexpr int T = kAttnThreads, NW = T / 64;
   constexpr int kSeg = kMaxRowSlots / (MODE == ROWS_SEL_TOKEN ? 16 : 1);   // groups listed at once
@@ -144,13 +147,13 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
   };
 
   // shared state of the attention of one piece
-  constexpr int kChunk = (kStageFloats / (G * 16)) / 16 * 16;
+  constexpr int kChunk = (kStageFloats<KV8> / (G * 16)) / 16 * 16;
   __shared__ __attribute__((aligned(16))) float s_stage[LOGITS ? kChunk * G * 16 : 1];
   __shared__ float s_m[NW][kMaxGroup], s_l[NW][kMaxGroup];
   // each wave's K tile on its way to the matrix cores, later its outputs; then the outputs of
   // the thread groups that merge partials
   union WaveSpace {
-    uint16_t k[16 * D];
+    uint16_t k[SG * 16 * D];
     float o[G][D];
   };
   __shared__ __attribute__((aligned(16))) WaveSpace s_w[NW];
@@ -241,15 +244,19 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
     stage_query_lds<D, G>(qb, s_qv[wave], lane);
     wave_lds_sync();
 #endif
-    auto process = [&](CacheTile& t, int slot_in_chunk) {
-      float* logit_slot = s_stage + slot_in_chunk * G * 16;
+    // a wave's groups k .. k + SG - 1, as far as below ke; slot_of: a group's place in the chunk
+    auto process = [&](CacheTile (&t)[SG], auto&& slot_of, int k, int ke) {
+      float* logit_slot = s_stage + slot_of(k) * G * 16;
+      if constexpr (KV8) {
+        float* const slots[2] = {logit_slot, k + 1 < ke ? s_stage + slot_of(k + 1) * G * 16 : nullptr};
+        process_pair<D, G, LOGITS>(t, qb, scale, st, s_w[wave].k, slots, lane);
+      } else {
 #if DELTA_QK_VALU
-      if constexpr (!KV8) {
-        process_tile_valu<D, G, LOGITS>(t, s_qv[wave], scale, st, s_p[wave], s_w[wave].k, logit_slot, lane);
-        return;
-      }
+        process_tile_valu<D, G, LOGITS>(t[0], s_qv[wave], scale, st, s_p[wave], s_w[wave].k, logit_slot, lane);
+#else
+        process_tile<D, G, LOGITS>(t[0], qb, scale, st, s_w[wave].k, logit_slot, lane);
 #endif
-      process_tile<D, G, LOGITS>(t, qb, scale, st, s_w[wave].k, logit_slot, lane);
+      }
     };
 
     // The waves take a piece's groups in turn: one at a time in short pieces, so that every wave
@@ -274,21 +281,30 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
       if (kb >= ke) return;
       // (the scheduler must not reorder the loads of different tiles: the compiler's wait for
       // the oldest tile would then drain the younger ones)
-      int row = s_rows[MODE == ROWS_SEL_TOKEN ? 0 : group_of(kb)];
-      auto fetch = [&](CacheTile& t, int k) {
+      int row[SG];
+#pragma unroll
+      for (int u = 0; u < SG; ++u) row[u] = s_rows[MODE == ROWS_SEL_TOKEN ? 0 : group_of(min(kb + u, ke - 1))];
+      auto fetch = [&](CacheTile (&t)[SG], int k) {
         __builtin_amdgcn_sched_barrier(0);
-        load_tile(t, row, group_of(min(k, ke - 1)), l0, k < ke);
-        if (MODE != ROWS_SEL_TOKEN) row = s_rows[group_of(min(k + 1, ke - 1))];
+#pragma unroll
+        for (int u = 0; u < SG; ++u) {
+          load_tile(t[u], row[u], group_of(min(k + u, ke - 1)), l0, k + u < ke);
+          if (KV8 && k + u >= ke) t[u].kmask = 0u;   // the second of a last, single group
+        }
+#pragma unroll
+        for (int u = 0; u < SG; ++u)
+          if (MODE != ROWS_SEL_TOKEN) row[u] = s_rows[group_of(min(k + SG + u, ke - 1))];
         __builtin_amdgcn_sched_barrier(0);
       };
-      CacheTile t[R];
+      auto slot_of = [&](int k) { return group_of(k) - c0; };
+      CacheTile t[R][SG];
 #pragma unroll
-      for (int i = 0; i < R - 1; ++i) fetch(t[i], kb + i);
-      for (int k = kb; k < ke; k += R) {
+      for (int i = 0; i < R - 1; ++i) fetch(t[i], kb + SG * i);
+      for (int k = kb; k < ke; k += SG * R) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          fetch(t[(r + R - 1) % R], k + r + R - 1);
-          if (k + r < ke) process(t[r], group_of(k + r) - c0);
+          fetch(t[(r + R - 1) % R], k + SG * (r + R - 1));
+          if (k + SG * r < ke) process(t[r], slot_of, k + SG * r, ke);
         }
       }
     };

@@ -88,13 +88,20 @@ struct Tile {
 // The same tile of an e4m3 cache as it comes from memory: half the words, expanded to bf16 (exactly:
 // an e4m3 value has 4 significant bits and exponents that bf16 has too) when the tile is consumed,
 // K on its way into the LDS slice, V in registers.  The expansion costs one instruction per two
-// values; what a wave keeps in flight are the 8-bit words, so R may be larger.
+// values; what a wave keeps in flight are the 8-bit words.  Two tiles are folded at a time: a wave's
+// chain of dependent steps is hardly longer for 32 rows than for 16 (one maximum, one branch, P.V by
+// v_mfma_f32_16x16x32_bf16 with half the MFMAs).  Measured on MI355X, us, one tile at a time (five in
+// the ring) and two: one 32K sequence with 28/4 heads 20.3 and 19.0; at the memory rate nothing, 32
+// ragged sequences of 16K-32K with 32/8 heads 276 and 275, a sparse layer of 16 sequences, 256 pages,
+// 27.4 and 27.3.  K loaded in the operand's layout without the LDS (lanes taking 16 of every 64 bytes of
+// their row): 19.4, 288 and 28.1.  Eight waves: 18.4-20.3, 278 and 28.5.
 template <int D>
 struct Geo8 {
   static constexpr int NL = D / 64;      // 16-byte K loads per lane per tile
   static constexpr int CPR = D / 16;     // 16-byte pieces of a K row
   static constexpr int RPL = 64 / CPR;   // K rows per wave-wide load
-  static constexpr int R = D == 128 ? 5 : 6;
+  // register ring, in pairs of tiles: the loads of R - 1 pairs stay in flight
+  static constexpr int R = D == 128 ? 3 : 4;
 };
 
 template <int D>
@@ -266,26 +273,32 @@ __device__ __forceinline__ void k_operand(const Tile<D>& t, uint16_t* lk, u32x4 
     ka[ks] = *reinterpret_cast<const u32x4*>(lk + k_slot<D>(lane & 15, 4 * ks + (lane >> 4)));
 }
 
-// The same from an e4m3 tile: each 16-byte piece of a row becomes two of the bf16 row.
+// The same from two e4m3 tiles (lk: two slices): each 16-byte piece of a row becomes two of the bf16
+// row.
 template <int D>
-__device__ __forceinline__ void k_operand(const Tile8<D>& t, uint16_t* lk, u32x4 (&ka)[Geo<D>::NK],
-                                          int lane) {
+__device__ __forceinline__ void k_operands(const Tile8<D> (&t)[2], uint16_t* lk,
+                                           u32x4 (&ka)[2][Geo<D>::NK], int lane) {
   using G8 = Geo8<D>;
   wave_lds_sync();
 #pragma unroll
-  for (int i = 0; i < G8::NL; ++i) {
-    const int r = G8::RPL * i + lane / G8::CPR, c = 2 * (lane % G8::CPR);
+  for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const u32x4 w = {e4m3x2_to_bf16x2<false>(t.k[i][2 * j]), e4m3x2_to_bf16x2<true>(t.k[i][2 * j]),
-                       e4m3x2_to_bf16x2<false>(t.k[i][2 * j + 1]), e4m3x2_to_bf16x2<true>(t.k[i][2 * j + 1])};
-      *reinterpret_cast<u32x4*>(lk + k_slot<D>(r, c + j)) = w;
+    for (int i = 0; i < G8::NL; ++i) {
+      const int r = G8::RPL * i + lane / G8::CPR, c = 2 * (lane % G8::CPR);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t a = t[u].k[i][2 * j], b = t[u].k[i][2 * j + 1];
+        *reinterpret_cast<u32x4*>(lk + u * 16 * D + k_slot<D>(r, c + j)) =
+            u32x4{e4m3x2_to_bf16x2<false>(a), e4m3x2_to_bf16x2<true>(a),
+                  e4m3x2_to_bf16x2<false>(b), e4m3x2_to_bf16x2<true>(b)};
+      }
     }
-  }
   wave_lds_sync();
 #pragma unroll
-  for (int ks = 0; ks < Geo<D>::NK; ++ks)
-    ka[ks] = *reinterpret_cast<const u32x4*>(lk + k_slot<D>(lane & 15, 4 * ks + (lane >> 4)));
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int ks = 0; ks < Geo<D>::NK; ++ks)
+      ka[u][ks] = *reinterpret_cast<const u32x4*>(lk + u * 16 * D + k_slot<D>(lane & 15, 4 * ks + (lane >> 4)));
 }
 
 // The V columns of an e4m3 tile in the layout of a bf16 tile.
@@ -410,22 +423,115 @@ __device__ __forceinline__ void process_tile(Tile<D>& t, const bf16x8 (&qb)[Geo<
   fold_tile<D, G, LOGITS>(acc, t, scale_log2, st, logit_slot, lane);
 }
 
-// The same for a tile of an e4m3 cache (scale_log2 includes the KV head's K scale).
+// The same for two tiles of an e4m3 cache (scale_log2 includes the KV head's K scale; a tile of
+// which no row exists has kmask 0).  As fold_tile, for 32 rows: tile u's probabilities are the terms
+// 4*u .. 4*u + 3 of the lane's eight in the P.V product, its V rows likewise.
 template <int D, int G, bool LOGITS>
-__device__ __forceinline__ void process_tile(Tile8<D>& raw, const bf16x8 (&qb)[Geo<D>::NK],
-                                             float scale_log2, WaveSoftmax<D, G>& st,
-                                             uint16_t* lk, float* logit_slot, int lane) {
-  u32x4 ka[Geo<D>::NK];
-  k_operand<D>(raw, lk, ka, lane);
-  Tile<D> t;
-  t.kmask = raw.kmask;
-  expand_v<D>(raw, t);
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ void process_pair(Tile8<D> (&raw)[2], const bf16x8 (&qb)[Geo<D>::NK],
+                                             float scale_log2, WaveSoftmax<D, G>& st, uint16_t* lk,
+                                             float* const (&logit_slot)[2], int lane) {
+#pragma clang fp contract(off)
+  using Gm = Geo<D>;
+  constexpr int S = kCopy<G>;
+  const int quad = lane >> 4, hcol = lane & 15;
+  u32x4 ka[2][Gm::NK];
+  k_operands<D>(raw, lk, ka, lane);
+  f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-  for (int ks = 0; ks < Geo<D>::NK; ++ks)
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[ks]), qb[ks],
-                                                  acc, 0, 0, 0);
-  fold_tile<D, G, LOGITS>(acc, t, scale_log2, st, logit_slot, lane);
+  for (int ks = 0; ks < Gm::NK; ++ks)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ka[u][ks]), qb[ks],
+                                                       acc[u], 0, 0, 0);
+  Tile<D> t[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) expand_v<D>(raw[u], t[u]);
+  const uint32_t kmask = __builtin_amdgcn_readfirstlane(raw[0].kmask | raw[1].kmask << 16);
+#pragma unroll
+  for (int u = 0; u < 2; ++u) acc[u] *= scale_log2;
+  if (kmask != 0xffffffffu) {   // rows past the end (their K and V may hold NaN)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const bool ok = (kmask >> (16 * u + 4 * quad + r)) & 1u;
+        acc[u][r] = ok ? acc[u][r] : kNegInfF;
+#pragma unroll
+        for (int w = 0; w < Gm::NW; ++w) t[u].v[r][w] = ok ? t[u].v[r][w] : 0u;
+      }
+  }
+  if (LOGITS && hcol < G) {
+    *reinterpret_cast<f32x4*>(logit_slot[0] + hcol * 16 + 4 * quad) = acc[0];
+    if (logit_slot[1]) *reinterpret_cast<f32x4*>(logit_slot[1] + hcol * 16 + 4 * quad) = acc[1];
+  }
+
+  float m_use = st.m_run, mx = fmaxf(acc[0][0], acc[1][0]);
+#pragma unroll
+  for (int r = 1; r < 4; ++r) mx = fmaxf(mx, fmaxf(acc[0][r], acc[1][r]));
+  if (__any(!(mx - m_use <= 0.f))) {
+    const float m_new = fmaxf(st.m_run, max_xor32(max_xor16(mx)));
+    m_use = (m_new == kNegInfF) ? 0.f : m_new;
+    const float alpha = exp2f(st.m_run - m_use);
+    st.m_run = m_new;
+    st.l_run *= alpha;
+    float row[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float lo = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(alpha), r));
+      const float hi = S == 8 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(alpha), 4 + r)) : lo;
+      row[r] = (quad & 1) ? hi : lo;
+    }
+#pragma unroll
+    for (int c = 0; c < Gm::NC; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st.o[c][r] *= row[r];
+  }
+
+  constexpr uint32_t kHigh = 0xffff0000u;
+  const uint32_t m1 = hcol >= S ? kHigh : 0u, m2 = hcol >= 2 * S ? kHigh : 0u;
+  auto high = [](float x, uint32_t m) { return __uint_as_float(__float_as_uint(x) & m); };
+  auto pack = [](float lo, float hi) {
+    return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+  };
+  const float part = S == 8 && hcol < S ? 0.5f : 1.f;
+  u32x4 pa, pb = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    float p[4], a1[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(acc[u][r] - m_use);
+    st.l_run += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      a1[r] = fmaf(p[r], part, -high(p[r], m1));
+      if (S == 4) a1[r] -= high(a1[r], m2);
+    }
+    pa[2 * u] = pack(a1[0], a1[1]);
+    pa[2 * u + 1] = pack(a1[2], a1[3]);
+    if (S == 8) {
+      float a2[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) a2[r] = a1[r] - high(a1[r], kHigh);
+      pb[2 * u] = hcol >= S ? pack(a2[0], a2[1]) : pa[2 * u];
+      pb[2 * u + 1] = hcol >= S ? pack(a2[2], a2[3]) : pa[2 * u + 1];
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < Gm::NC; ++c) {
+    const uint32_t pick = (c & 1) ? 0x07060302u : 0x05040100u;
+    const int w = c / 2;
+    u32x4 vb;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      vb[2 * u] = __builtin_amdgcn_perm(t[u].v[1][w], t[u].v[0][w], pick);
+      vb[2 * u + 1] = __builtin_amdgcn_perm(t[u].v[3][w], t[u].v[2][w], pick);
+    }
+    st.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pa),
+                                                      __builtin_bit_cast(bf16x8, vb), st.o[c], 0, 0, 0);
+    if (S == 8)
+      st.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, pb),
+                                                        __builtin_bit_cast(bf16x8, vb), st.o[c], 0, 0, 0);
+  }
 }
 
 // The same score tile with QK^T on the vector ALUs, a build option (DELTA_QK_VALU) kept for
