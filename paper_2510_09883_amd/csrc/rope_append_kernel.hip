@@ -5,10 +5,14 @@
 // The angle p f of a far position has an fp32 rounding error of 2^-24 p f (0.008 radians at 131072),
 // so it is formed in fp64 and reduced there to [-pi, pi] before the fp32 sine and cosine.
 //
-// Work.  A workgroup takes `tokens` rows.  Wave w finds row w's sequence, position and place in
+// Work.  A workgroup takes `tokens` rows (see launch_rope_append).  Wave w finds row w's sequence, position and place in
 // the cache, and its lanes the cosines and sines of the row's at most 64 angles, once for all
 // heads, into LDS.  Then every thread takes units of 16 head elements: two 16-byte loads, the
 // rotation, two 16-byte stores (8-byte ones to an e4m3 cache).
+//
+// Bound: the copy rate for prompts (86423 rows of 40/8 heads into an e4m3 cache, 2.3 GB in 431 us, 5.3
+// TB/s, where a plain copy runs at 5.0), launch and the chain of lookups (offset, length, page) for a
+// few rows (one row 3.6 us in a graph).
 #include "debug_check.h"
 #include "runs.h"
 
@@ -163,7 +167,14 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeAppendA
 }  // namespace
 
 hipError_t launch_rope_append(int head_dim, bool kv8, const RopeAppendArgs& a, hipStream_t stream) {
-  const int tokens = kMaxTokens;
+  // One row a workgroup: rows are then looked up and their angles formed in parallel.  Several share
+  // one only where a row leaves most of the threads idle and there are rows enough to fill the device.
+  // Measured on MI355X, us, one and four rows a workgroup: 64 rows of 32/8 heads 3.9 and 6.2, 1024 6.1
+  // and 7.5, 8192 31.6 and 33.0; of 12/2 heads (128 units) 64 rows 3.2 and 3.8, 8192 14.4 and 12.7.
+  // (Loading a thread's first units before its row is known: 64 rows of 12/2 heads 4.0 -> 4.5, 9351 of
+  // 32/8 35.9 -> 37.8, 86423 of 40/8 431 -> 425; non-temporal loads 456 -> 501 there.)
+  const int units = (a.n_q_heads + 2 * a.n_kv_heads) * (head_dim / 16);
+  const int tokens = units <= kThreads / 2 && a.runs.n_rows >= 4096 ? kMaxTokens : 1;
   const dim3 grid((a.runs.n_rows + tokens - 1) / tokens), block(kThreads);
   if (head_dim == 128) {
     if (kv8) hipLaunchKernelGGL((rope_append_kernel<128, true>), grid, block, 0, stream, a, tokens);
