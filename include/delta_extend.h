@@ -59,8 +59,9 @@ int delta_rope_append(const delta_shape_t* shape, const delta_kv_t* kv, const de
                       int64_t q_row_stride, const void* k, int64_t k_row_stride, const void* v,
                       int64_t v_row_stride, void* q_out, void* stream);
 
-/* Bytes of workspace that delta_extend_attn needs for this shape, number of rows and longest run.
- * Host only. */
+/* Bytes of workspace that are enough for delta_extend_attn with this shape, for every call of at
+ * most n_rows rows and runs of at most max_new (host only): 4 (head_dim + 3) bytes and a little per
+ * part of an output, of which a call keeps at most 32 per row and query head and 131072 in all. */
 int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int32_t max_new,
                                  size_t* out);
 
@@ -73,8 +74,10 @@ int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int
  *            undefined)
  *   ws:      at least delta_extend_workspace_bytes() bytes, 256-byte aligned, of any content;
  *            it keeps nothing between calls.  Calls that share one must not run concurrently.
+ *            (A debug build's status word is its first: zero it before the call to read it.)
  * seq_lens[b] may be 0 (with an empty run) and is cut to max_seq_len.  Keys and
  * values of a sequence's tokens are finite; whatever else a page holds is not looked at.
+ * A query that is NaN gives NaN in its own outputs only.
  * bf16 queries, fp32 scores, softmax and sums, one bf16 rounding of the result; where a kernel
  * works on whole tiles of rows (see max_new) the probabilities are rounded to bf16 before they
  * meet the values (at most 2^-8 of each), their sum is not.  Deterministic: the same call

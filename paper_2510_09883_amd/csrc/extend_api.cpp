@@ -9,6 +9,11 @@
 
 namespace delta {
 
+// Most pieces that a call's keys are cut into, and most (row, query head) parts of outputs that it
+// keeps (68 MB at head size 128): with the second a call's workspace grows with its rows and nothing
+// else, so that one sized for the most rows serves every smaller call.
+constexpr int kMostSplits = 32, kMostParts = 1 << 17;
+
 // Which kernel, and into how many pieces the keys are cut.  The host knows no run but the longest, so
 // it takes the rows for runs of that length and single tokens.
 //
@@ -22,7 +27,7 @@ namespace delta {
 // 303 and 168; 256 tokens behind a prefix of 7936 93 and 55; eight prompts of 256 35 and 20; eight
 // times 16 tokens at 4096 37 and 36.
 ExtendPlan plan_extend(const delta_shape_t* s, int n_rows, int max_new) {
-  constexpr int kCus = 256, kMostSplits = 32, kFewestKeys = 256, kStart = 4;
+  constexpr int kCus = 256, kFewestKeys = 256, kStart = 4;
   const int G = s->n_q_heads / s->n_kv_heads;
   const double keys = s->max_seq_len;
   const int spare = std::max(0, n_rows - s->batch);   // rows beyond one per sequence
@@ -34,7 +39,8 @@ ExtendPlan plan_extend(const delta_shape_t* s, int n_rows, int max_new) {
   auto cut = [&](int rows, double light, double keys_per_unit) {
     const double tiles = runs * ceil((double)max_new * G / rows) + light * (s->batch - runs);
     const double wgs = std::max(1.0, tiles * s->n_kv_heads);
-    const int splits = (int)std::max(1.0, std::min({kCus / wgs, (double)kMostSplits, keys / kFewestKeys}));
+    const double parts = (double)kMostParts / std::max<int64_t>(1, (int64_t)n_rows * s->n_q_heads);
+    const int splits = (int)std::max(1.0, std::min({kCus / wgs, (double)kMostSplits, keys / kFewestKeys, parts}));
     return Cut{keys / keys_per_unit / splits * std::max(1.0, wgs * splits / kCus), splits};
   };
   const Cut few = cut(32, 1.0, 128), many = cut(256, 0.25, 32);
@@ -72,25 +78,31 @@ Runs runs_of(const delta_shape_t* s, const delta_kv_t* kv, int32_t n_rows, const
 
 struct ExtendLayout {
   ExtendPlan plan;
+  int n_rows = 0;   // rows that can belong to a run
   size_t status = 0, part_ml = 0, part_n = 0, part_o = 0, total = 0;
 };
+
+// Bytes of `rows` (row, query head) pairs in `parts` parts.
+size_t lay_out(size_t rows, size_t parts, int head_dim, ExtendLayout* L) {
+  size_t off = 0;
+  L->status = off;  off = align_up(off + sizeof(uint32_t));
+  L->part_ml = off; off = align_up(off + sizeof(float) * 2 * parts);
+  L->part_n = off;  off = align_up(off + sizeof(int32_t) * rows);
+  L->part_o = off;  off = align_up(off + sizeof(float) * head_dim * parts);
+  return off;
+}
 
 int extend_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, ExtendLayout* L) {
   int rc = check_shape(s);
   if (rc) return rc;
   if (n_rows < 0 || max_new < 0 || max_new > n_rows) return DELTA_ERR_INVALID_ARG;
   if ((int64_t)n_rows * s->n_q_heads > (1 << 28)) return DELTA_ERR_UNSUPPORTED;
-  L->plan = plan_extend(s, n_rows, max_new);
+  L->n_rows = (int)std::min<int64_t>(n_rows, (int64_t)s->batch * max_new);
+  L->plan = plan_extend(s, L->n_rows, max_new);
   if (L->plan.tiles > 65535) return DELTA_ERR_UNSUPPORTED;
-  size_t off = 0;
-  L->status = off; off = align_up(off + sizeof(uint32_t));
-  if (L->plan.n_split > 1) {
-    const size_t parts = (size_t)L->plan.n_split * n_rows * s->n_q_heads;
-    L->part_ml = off; off = align_up(off + sizeof(float) * 2 * parts);
-    L->part_n = off;  off = align_up(off + sizeof(int32_t) * (size_t)n_rows * s->n_q_heads);
-    L->part_o = off;  off = align_up(off + sizeof(float) * s->head_dim * parts);
-  }
-  L->total = off;
+  const size_t rows = (size_t)L->n_rows * s->n_q_heads;
+  if (L->plan.n_split > 1) L->total = lay_out(rows, L->plan.n_split * rows, s->head_dim, L);
+  else L->total = lay_out(0, 0, s->head_dim, L);
   return DELTA_OK;
 }
 
@@ -153,7 +165,8 @@ int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int
   ExtendLayout L;
   int rc = extend_layout(shape, n_rows, max_new, &L);
   if (rc) return rc;
-  *out = L.total;
+  const size_t rows = (size_t)L.n_rows * shape->n_q_heads, most = kMostParts;
+  *out = lay_out(std::min(rows, most), std::min(kMostSplits * rows, most), shape->head_dim, &L);
   return DELTA_OK;
 }
 
@@ -175,7 +188,7 @@ int delta_extend_attn(const delta_shape_t* shape, const delta_kv_t* kv, int32_t 
   if (!aligned(ws, 256)) return DELTA_ERR_INVALID_ARG;
   char* w = static_cast<char*>(ws);
   ExtendArgs a{};
-  a.runs = runs_of(shape, kv, n_rows, row_offsets);
+  a.runs = runs_of(shape, kv, L.n_rows, row_offsets);
   a.k_cache = static_cast<const uint8_t*>(kv->k_cache);
   a.v_cache = static_cast<const uint8_t*>(kv->v_cache);
   a.k_scale = kv->k_scale;

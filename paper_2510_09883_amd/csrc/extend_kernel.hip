@@ -57,7 +57,7 @@ __device__ __forceinline__ u32x2 pack_outputs(const f32x4& x, float scale, float
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const float a = x[2 * k] * scale, b = x[2 * k + 1] * scale;
-    const bf16x2 p = {(__bf16)(l > 0.f ? a / l : 0.f), (__bf16)(l > 0.f ? b / l : 0.f)};
+    const bf16x2 p = {(__bf16)(l == 0.f ? 0.f : a / l), (__bf16)(l == 0.f ? 0.f : b / l)};
     w[k] = __builtin_bit_cast(uint32_t, p);
   }
   return w;
@@ -357,23 +357,36 @@ template <int ROWS>
 __device__ __forceinline__ bool find_tile(const ExtendArgs& a, TileOf& t) {
   const int lane = threadIdx.x & 63, G = a.n_q_heads / a.n_kv_heads;
   int tile = blockIdx.y;
-  for (int c = 0; c < a.runs.batch; c += 64) {
-    int lo = 0, len = 0;
-    if (c + lane < a.runs.batch) {
-      lo = run_offset(a.runs, c + lane);
-      len = max(0, run_offset(a.runs, c + lane + 1) - lo);
+  // 256 sequences a round, four neighbours per lane
+  constexpr int kPer = 4;
+  for (int c = 0; c < a.runs.batch; c += 64 * kPer) {
+    int at[kPer + 1], tiles[kPer], sum = 0;
+#pragma unroll
+    for (int i = 0; i <= kPer; ++i) at[i] = run_offset(a.runs, min(c + kPer * lane + i, a.runs.batch));
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      tiles[i] = (int)(((int64_t)max(0, at[i + 1] - at[i]) * G + ROWS - 1) / ROWS);
+      sum += tiles[i];
     }
-    const int tiles = (int)(((int64_t)len * G + ROWS - 1) / ROWS);
-    const int incl = wave_incl_scan(tiles);
+    const int incl = wave_incl_scan(sum);
     const uint64_t past = __ballot(incl > tile);
     if (past) {
       const int l = __builtin_ctzll(past);
-      t.b = c + l;
-      t.begin = __builtin_amdgcn_readlane(lo, l);
-      t.n_new = __builtin_amdgcn_readlane(len, l);
+      int left = tile - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(sum, l));
+      bool found = false;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int n = __builtin_amdgcn_readlane(tiles[i], l);
+        if (!found && left < n) {
+          found = true;
+          t.b = c + kPer * l + i;
+          t.begin = __builtin_amdgcn_readlane(at[i], l);
+          t.n_new = __builtin_amdgcn_readlane(at[i + 1], l) - t.begin;
+          t.first = (n - 1 - left) * ROWS;   // the last rows see most keys: they start first
+        }
+        left -= found ? 0 : n;
+      }
       t.n_rows = t.n_new * G;   // (n_rows * Hq < 2^31)
-      // the last rows see most keys: they start first
-      t.first = (__builtin_amdgcn_readlane(incl, l) - 1 - tile) * ROWS;
       t.s_b = max(0, min(a.runs.seq_lens[t.b], a.max_seq_len));
       return true;
     }
@@ -415,8 +428,9 @@ __global__ __launch_bounds__(256) void extend_join_kernel(const ExtendArgs a, bo
   const int row = (int)(item / Hq), head = (int)(item - (int64_t)row * Hq);
   if (row < first || row >= end) return;
   const size_t stride = (size_t)a.runs.n_rows * Hq;
-  const int n = a.part_n[item];   // 0: written by its only piece
-  if (n == 0) return;
+  // 0: written by its only piece.  (Bounded: a run longer than the host's bound has rows without.)
+  const int n = min(a.part_n[item], a.n_split);
+  if (n <= 0) return;
   float m = kNegInfF, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int s = 0; s < n; ++s) {

@@ -65,10 +65,10 @@ def _offsets(row_offsets, batch):
         _dev("row_offsets", row_offsets, torch.int32, (batch + 1,))
 
 
-def _stream_of(*tensors):
-    """The current device's current stream; every tensor has to be on that device."""
+def _stream_of(kv, *tensors):
+    """The current device's current stream; the cache and every tensor have to be on that device."""
     here = torch.cuda.current_device()
-    for t in tensors:
+    for t in (*tensors, *getattr(kv, "_tensors", ())[:1]):
         if t is not None and t.get_device() != here:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
     return torch._C._cuda_getCurrentRawStream(here)
@@ -103,7 +103,7 @@ def delta_rope_append(shape, kv: delta_kv_t, q, k, v, q_out, inv_freq=None, row_
                                          1 if interleaved else 0))
     elif positions is not None:
         raise ValueError("positions: nothing is rotated without inv_freq")
-    stream = _stream_of(k, v, q, q_out, row_offsets, inv_freq, positions)
+    stream = _stream_of(kv, k, v, q, q_out, row_offsets, inv_freq, positions)
     _check("delta_rope_append",
            delta._lib.delta_rope_append(ctypes.byref(shape), ctypes.byref(kv), rope, n, _ptr(row_offsets),
                                         _ptr(q), qs, k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q_out), stream))
@@ -117,7 +117,8 @@ def delta_extend_workspace_bytes(shape: delta_shape_t, n_rows: int, max_new: int
 
 
 def alloc_extend_workspace(shape, n_rows, max_new, device="cuda") -> torch.Tensor:
-    """A workspace (uint8) large enough for delta_extend_attn calls of this shape."""
+    """A workspace (uint8) large enough for delta_extend_attn calls of this shape, with at most so many
+    rows and runs of at most max_new."""
     return torch.zeros(delta_extend_workspace_bytes(shape, n_rows, max_new), dtype=torch.uint8, device=device)
 
 
@@ -129,7 +130,7 @@ def delta_extend_attn(shape, kv: delta_kv_t, q, out, row_offsets, max_new, ws):
     _dev("out", out, torch.bfloat16, tuple(q.shape))
     _offsets(row_offsets, shape.batch)
     _dev("ws", ws)
-    stream = _stream_of(q, out, row_offsets, ws)
+    stream = _stream_of(kv, q, out, row_offsets, ws)
     _check("delta_extend_attn",
            delta._lib.delta_extend_attn(ctypes.byref(shape), ctypes.byref(kv), q.shape[0], max_new,
                                         _ptr(row_offsets), _ptr(q), _ptr(out), _ptr(ws), _nbytes(ws), stream))

@@ -66,12 +66,20 @@ def test_extend_arguments(kw, rc):
     assert extend(**kw) == rc
 
 
-def test_workspace_covers_the_splits():
-    """Few rows of a long cache keep parts of their outputs; a large prompt needs none."""
-    long = shape(batch=1, max_pages_per_seq=8192, max_seq_len=131072)
-    assert D.delta_workspace_bytes(long) > 0
-    few, many = E.delta_extend_workspace_bytes(long, 1, 1), E.delta_extend_workspace_bytes(shape(), 65536, 32768)
-    assert few >= 2 * 8 * 130 * 4 and many == 256
-    assert few % 256 == 0
+def test_workspace_grows_with_the_rows_alone():
+    """One sized for the most rows serves every smaller call, whatever its runs and lengths: the library
+    accepts it (a call of null queries gets past the workspace check and is refused after it)."""
+    part = 4 * (128 + 2)
+    for batch, held in ((1, 131072), (4, 1024), (64, 20000), (300, 64)):
+        s = shape(batch=batch, max_pages_per_seq=8192, max_seq_len=held)
+        sizes = [E.delta_extend_workspace_bytes(s, n, min(n, m)) for n, m in ((1, 1), (5, 3), (700, 700), (9000, 9000))]
+        assert sizes == sorted(sizes) and all(x % 256 == 0 for x in sizes)
+        assert sizes[-1] <= 131072 * (part + 4) + 2048
+        for n in (1, 2, 7, 40, 64, 300, 500, 1000, 4096, 9000):
+            for m in sorted({1, 2, 9, n // 2, n} - {0}):
+                if m <= n:
+                    assert extend(s=s, n_rows=n, max_new=m, q=None, ws_bytes=sizes[-1]) == -1
+                    assert extend(s=s, n_rows=n, max_new=m, q=None,
+                                  ws_bytes=E.delta_extend_workspace_bytes(s, n, m)) == -1
     with pytest.raises(D.DeltaError):
         E.delta_extend_workspace_bytes(shape(n_kv_heads=1, n_q_heads=16), 1, 1)

@@ -111,6 +111,29 @@ def test_many_sequences():
     c.check()
 
 
+@pytest.mark.parametrize("batch", [65, 256, 257, 700])
+def test_batches_around_what_a_lane_holds(batch):
+    """Runs of every length around the tile, empty ones among them, and one long one at the end."""
+    lens = [(17 * b) % 50 + 4 for b in range(batch)]
+    new = [(b * 5) % 5 - 1 if b % 3 else 0 for b in range(batch)]
+    new = [max(0, n) for n in new]
+    lens[-1], new[-1] = 90, 80
+    c = Call(lens, new, 4, 2, 64, seed=batch, pad=3)
+    c.run()
+    c.check(some=4)
+
+
+def test_a_query_of_nan_spoils_its_own_outputs_only():
+    for new in (3, 90):
+        c = Call([120], [new], 8, 2, 128, seed=52)
+        c.gpu[1, 2] = float("nan")
+        c.run()
+        torch.cuda.synchronize()
+        assert bool(c.out[1, 2].isnan().all())
+        c.out[1, 2] = 0
+        assert not bool(c.out.isnan().any())
+
+
 def test_single_tokens_without_offsets_match_the_decode_layer():
     lens = [1, 31, 500, 1024]
     c = Call(lens, [1] * 4, 8, 2, 128, seed=43, offsets=False)

@@ -139,6 +139,22 @@ def test_many_sequences_single_tokens_and_explicit_positions(e4m3, packed):
     c.check()
 
 
+@pytest.mark.parametrize("batch", [64, 65, 300, 4097])
+def test_rows_are_found_among_many_sequences(batch):
+    """Empty runs between others, at every size of the search for a row's sequence."""
+    new = [(b * 7 + 1) % 3 for b in range(batch)]
+    c = Call([n + b % 5 for b, n in enumerate(new)], new, 2, 1, 64, 16, seed=batch, pad=2)
+    c.run()
+    c.check()
+
+
+def test_large_prompts_share_workgroups():
+    """Few heads and many rows: several rows a workgroup, the last one partly filled."""
+    c = Call([4500, 600], [4500, 599], 2, 1, 64, 64, seed=15, pad=3)
+    c.run()
+    c.check()
+
+
 @pytest.mark.parametrize("base", [1.0, 10000.0, 1e6])
 def test_far_positions(base):
     """Angles up to 131071 radians: an fp32 angle would be off by 0.004."""
