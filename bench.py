@@ -938,7 +938,7 @@ def main():
     logits = "true" if dominant == "delta" else "false"
     # dense launches over 2-64 sequences run the balanced instantiation
     balanced = "true" if mode == 0 and 2 <= w.batch <= 64 else "false"
-    kernel_tag = f"attn_kernel<{w.head_dim}, {w.group}, {mode}, {logits}, {balanced}>"
+    kernel_tag = f"attn_kernel<{w.head_dim}, {w.group}, {mode}, {logits}, {balanced}, false>"   # bf16 caches
     traffic = measured_traffic(dominant, w, kernel_tag)
     achieved = role_bytes[dominant] / (layer_us[dominant] * 1e-6) / 1e9
     overhead = (layer_us["delta"] - layer_us["full"]) / layer_us["full"] if "delta" in layer_us and "full" in layer_us else None

@@ -8,10 +8,19 @@
 //
 // Work.  The rows of a run that share a KV head (token-major, the group's query heads next to each
 // other) are cut into tiles; a workgroup takes a tile, and one of n_split pieces of the keys that
-// the tile's last row sees.  It walks them in blocks that all its waves bring to LDS, 16 bytes a
-// thread and load, the next block's loads in flight (in registers) while one is worked on.  A wave
-// holds 32 rows and takes 32*KT keys of a block; WR waves stand along the rows, WK along the keys.
+// the tile's last row sees (extend_api.cpp decides the cut).  A wave holds 32 rows and takes 32*KT
+// keys of a block; WR waves stand along the rows, WK along the keys.  Two kernels:
 //
+//   * many rows: tiles of 256, eight waves along the rows (WR = 8).  All waves bring a block of 64
+//     keys to LDS, 16 bytes a thread and load; the next block's loads are in flight, in registers,
+//     while one is worked on; two buffers, one barrier a block.  A tile of at most 32 rows (a single
+//     token beside prompts) is taken as below, by all eight waves along its keys.
+//   * few rows: tiles of 32, four waves along the keys (WK = 4).  Waves share nothing, so each brings
+//     its own 32 keys to its own LDS, without barriers, loads the bytes past the caches, and two
+//     workgroups fit a CU.  In the end the waves are joined through LDS, each taking a share of the
+//     outputs.
+//
+// Per 32 keys and wave:
 //   * S^T = K Q^T by v_mfma_f32_32x32x16_bf16 with A = 32 keys, B = the 32 rows' queries (in
 //     registers throughout).  Lane (h, n) = (lane / 32, lane % 32) gets row n's scores of keys
 //     8*(i/4) + 4*h + i%4, i = 0 .. 15: a row lives in two lanes, so that its maximum and sum are
@@ -24,7 +33,23 @@
 //
 // LDS layouts: K rows with their 16-byte pieces permuted by the row (16 lanes reading one piece of
 // 16 rows touch all banks), V rows with their 64-byte pieces permuted by the row (the four rows of
-// a transposing read do).
+// a transposing read do).  The counters show no bank conflict.
+//
+// Precision.  Scores, maximum, sum and outputs are fp32; a probability is rounded to bf16 for the
+// P V product, whose inputs the matrix cores take in 16 bits: at most 2^-8 of each, which in the
+// output adds to the result's own rounding (1.7e-3 rms together instead of 1.6e-3).  Three bf16 terms
+// per probability, as the decode kernel has them for free in idle columns, would double the products.
+//
+// Bound.  Many rows: the card's power, then the issue of two waves a SIMD.  A prompt of 8192 tokens,
+// 32/8 heads: 580-640 us from card to card (860-950 TFLOP/s, where the library's product of 8192 x 8192
+// random matrices runs at 1450); 503 with every value zero, at which that product runs at 2100.  The
+// products alone take 356 us; reading K and V from LDS 130 of the rest, exponents and maxima 140, moving
+// blocks to LDS 90, the barrier 30.  Measured slower or equal: scores of the next 32 keys formed during
+// the softmax of these (636), blocks passed by counters instead of a barrier (654), 128-row tiles with
+// two workgroups a CU (645), 64 rows a wave, which halves the LDS reads but moves the queries through
+// accumulation registers (820), raised priority around the products (635).
+// Few rows: HBM, 16 sequences of 4K-16K tokens with up to 8 drafted ones, 32/8 heads, 709 MB: 119 us (6.0
+// TB/s) and 4.6 for the join; with ordinary loads 148.
 #include <algorithm>
 
 #include "attn_tile.h"

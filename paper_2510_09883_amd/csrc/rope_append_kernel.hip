@@ -5,10 +5,10 @@
 // The angle p f of a far position has an fp32 rounding error of 2^-24 p f (0.008 radians at 131072),
 // so it is formed in fp64 and reduced there to [-pi, pi] before the fp32 sine and cosine.
 //
-// Work.  A workgroup takes `tokens` rows (see launch_rope_append).  Wave w finds row w's sequence, position and place in
-// the cache, and its lanes the cosines and sines of the row's at most 64 angles, once for all
-// heads, into LDS.  Then every thread takes units of 16 head elements: two 16-byte loads, the
-// rotation, two 16-byte stores (8-byte ones to an e4m3 cache).
+// Work.  A workgroup takes `tokens` rows (see launch_rope_append).  Wave w finds row w's sequence,
+// position and place in the cache, and its lanes the cosines and sines of the row's at most 64
+// angles, once for all heads, into LDS.  Then every thread takes units of 16 head elements: two
+// 16-byte loads, the rotation, two 16-byte stores (8-byte ones to an e4m3 cache).
 //
 // Bound: the copy rate for prompts (86423 rows of 40/8 heads into an e4m3 cache, 2.3 GB in 431 us, 5.3
 // TB/s, where a plain copy runs at 5.0), launch and the chain of lookups (offset, length, page) for a
