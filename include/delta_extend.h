@@ -75,9 +75,10 @@ int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int
  *   ws:      at least delta_extend_workspace_bytes() bytes, 256-byte aligned, of any content;
  *            it keeps nothing between calls.  Calls that share one must not run concurrently.
  *            (A debug build's status word is its first: zero it before the call to read it.)
- * seq_lens[b] may be 0 (with an empty run) and is cut to max_seq_len.  Keys and
- * values of a sequence's tokens are finite; whatever else a page holds is not looked at.
- * A query that is NaN gives NaN in its own outputs only.
+ * seq_lens[b] may be 0 (with an empty run) and is cut to max_seq_len.
+ * What a row does not see does not reach it, infinite and NaN keys and values of later tokens and of
+ * rows past the sequence among it; those that it sees can make its outputs infinite or NaN (a value
+ * its own element, a key all), and a NaN query its own outputs.
  * bf16 queries, fp32 scores, softmax and sums, one bf16 rounding of the result; where a kernel
  * works on whole tiles of rows (see max_new) the probabilities are rounded to bf16 before they
  * meet the values (at most 2^-8 of each), their sum is not.  Deterministic: the same call

@@ -74,6 +74,26 @@ __device__ __forceinline__ int v_at(int r, int e) {
   return r * D + (e ^ (D == 128 ? (r & 3) << 5 : ((r >> 1) & 1) << 5));
 }
 
+// Infinite and NaN values among two bf16 (all exponent bits set) or four e4m3 (NaN: all bits but the
+// sign's set): `seen` gathers what tells of them, has_others reads it, without_others makes them 0.
+template <bool KV8>
+__device__ __forceinline__ void look_for_others(uint32_t w, uint32_t& seen) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  if (KV8) seen |= (w & 0x7f7f7f7fu) + 0x01010101u;
+  else
+    seen = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, seen),
+                                                                  __builtin_bit_cast(u16x2, w & 0x7fff7fffu)));
+}
+template <bool KV8>
+__device__ __forceinline__ bool has_others(uint32_t seen) {
+  return KV8 ? (seen & 0x80808080u) != 0 : (seen >> 16) >= 0x7f80u || (seen & 0xffffu) >= 0x7f80u;
+}
+template <bool KV8>
+__device__ __forceinline__ uint32_t without_others(uint32_t w) {
+  if (KV8) return w & ~(((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu);
+  return w & ~(((((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu);
+}
+
 // Four outputs, scaled and divided by the softmax sum, as bf16; a row that sees no key (l = 0) gets
 // zeros.  (Divided: a product by 1 / l has a rounding more, which moves quotients half way between
 // two bf16 values, as equal weights give.)
@@ -103,7 +123,8 @@ template <int D, int WR, int WK, int KT>
 constexpr int kBodyLds = std::max(2 * (WR == 1 ? 1 : 2) * 32 * KT * WK * D * 2, WK > 1 ? WK * 64 * D / 2 * 4 : 0);
 
 template <int D, int WR, int WK, int KT, bool KV8>
-__device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t, uint16_t* s_kv, float2* s_ml) {
+__device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t, uint16_t* s_kv, float2* s_ml,
+                                            int* s_others) {
   constexpr int NW = WR * WK, T = 64 * NW;
   constexpr int BM = 32 * WR;           // rows of a tile
   constexpr int BK = 32 * KT;           // keys a wave takes of a block
@@ -191,16 +212,39 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
       vr[i] = kOwnKeys ? __builtin_nontemporal_load(vp) : *vp;
     }
   };
+  // Where some rows of the tile do not see all keys of a block (an edge block; only there do keys lie
+  // past the sequence), 0 times a value that is infinite or NaN would reach rows that do not see its
+  // token: such values go to LDS as 0, and the rows that do see them get them at the end.  (Looking for
+  // them takes 0.2 us of 7.2 where every block is an edge block, 8 short sequences, else no time seen;
+  // replacing them without looking took 0.6.)
+  const int lim_first = lim_of(t.first);
+  bool others = false;   // the wave has met such values
   auto store = [&](int blk, int buf) {
     uint16_t* sk = s_kv + buf * 2 * kBlock;
     uint16_t* sv = sk + kBlock;
+    if ((blk + 1) * BN > lim_first) {
+      uint32_t seen = 0;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        if (kPieces % T && row_of(i) >= BN) break;
+        if (blk * BN + row_of(i) + lane / CPR >= s_b) vr[i] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) look_for_others<KV8>(vr[i][w], seen);
+      }
+      if (__any(has_others<KV8>(seen))) {
+        others = true;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          if (kPieces % T && row_of(i) >= BN) break;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) vr[i][w] = without_others<KV8>(vr[i][w]);
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int row = row_of(i) + lane / CPR, c = lane % CPR;
       if (kPieces % T && row >= BN) break;
-      u32x4 v = vr[i];
-      // rows past the sequence: 0 times what they hold (NaN) would spoil the sums
-      if (blk * BN + row >= s_b) v = u32x4{0u, 0u, 0u, 0u};
       if constexpr (KV8) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -209,15 +253,15 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
           for (int w = 0; w < 2; ++w) {
             wk[2 * w] = e4m3x2_to_bf16x2<false>(kr[i][2 * half + w]);
             wk[2 * w + 1] = e4m3x2_to_bf16x2<true>(kr[i][2 * half + w]);
-            wv[2 * w] = e4m3x2_to_bf16x2<false>(v[2 * half + w]);
-            wv[2 * w + 1] = e4m3x2_to_bf16x2<true>(v[2 * half + w]);
+            wv[2 * w] = e4m3x2_to_bf16x2<false>(vr[i][2 * half + w]);
+            wv[2 * w + 1] = e4m3x2_to_bf16x2<true>(vr[i][2 * half + w]);
           }
           *reinterpret_cast<u32x4*>(sk + k_at<D>(row, 2 * c + half)) = wk;
           *reinterpret_cast<u32x4*>(sv + v_at<D>(row, 16 * c + 8 * half)) = wv;
         }
       } else {
         *reinterpret_cast<u32x4*>(sk + k_at<D>(row, c)) = kr[i];
-        *reinterpret_cast<u32x4*>(sv + v_at<D>(row, 8 * c)) = v;
+        *reinterpret_cast<u32x4*>(sv + v_at<D>(row, 8 * c)) = vr[i];
       }
     }
   };
@@ -319,6 +363,33 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
     }
   }
   l = sum_xor32(l);
+
+  // ---- infinite and NaN values of edge blocks, to the rows that see them (the weight of a token that a
+  // row sees is positive, so they are what they add up to)
+  if constexpr (!kOwnKeys) {
+    if (others) *s_others = 1;
+    lds_barrier();
+    others = *s_others != 0;
+  }
+  if (others) {
+#pragma unroll 1
+    for (int blk = max(blk0, lim_first / BN); blk < blk1; ++blk)
+#pragma unroll 1
+      for (int key = blk * BN + wk * BK; key < min(blk * BN + (wk + 1) * BK, lim_hi); ++key) {
+        const int page = checked_page(table[key >> 4], a.n_pages, a.status);
+        const uint8_t* v = a.v_cache + ((size_t)page * a.page_stride + (size_t)(g * 16 + key % 16) * D) * EB;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int e = 32 * d + 8 * (i / 4) + 4 * h + i % 4;
+            uint32_t bits;   // as fp32
+            if constexpr (KV8) bits = (v[e] & 0x7f) == 0x7f ? 0x7fc00000u : 0u;
+            else bits = (uint32_t)reinterpret_cast<const uint16_t*>(v)[e] << 16;
+            if (key < lim && (bits & 0x7f800000u) == 0x7f800000u) o[d][i] += __uint_as_float(bits);
+          }
+      }
+  }
 
   // ---- the result, or this split's part of it: outputs e .. e + 3 of the lane's row ----------
   const float v_scale = KV8 && a.v_scale ? a.v_scale[g] : 1.f;
@@ -426,7 +497,7 @@ __global__ __launch_bounds__(256, 2) void extend_few_kernel(const ExtendArgs a) 
   __shared__ __attribute__((aligned(256))) uint16_t s_kv[kBodyLds<D, 1, 4, 1> / 2];
   __shared__ float2 s_ml[4 * 64];
   TileOf t;
-  if (find_tile<32>(a, t)) extend_body<D, 1, 4, 1, KV8>(a, t, s_kv, s_ml);
+  if (find_tile<32>(a, t)) extend_body<D, 1, 4, 1, KV8>(a, t, s_kv, s_ml, nullptr);
 }
 
 // Tiles of 256 rows, eight waves along them; a tile that has no more than 32 (a single token beside
@@ -435,10 +506,12 @@ template <int D, bool KV8>
 __global__ __launch_bounds__(512, 1) void extend_many_kernel(const ExtendArgs a) {
   __shared__ __attribute__((aligned(256))) uint16_t s_kv[std::max(kBodyLds<D, 8, 1, 2>, kBodyLds<D, 1, 8, 1>) / 2];
   __shared__ float2 s_ml[8 * 64];
+  __shared__ int s_others;   // some wave has met infinite or NaN values in an edge block
   TileOf t;
   if (!find_tile<256>(a, t)) return;
-  if (t.n_rows - t.first <= 32) extend_body<D, 1, 8, 1, KV8>(a, t, s_kv, s_ml);
-  else extend_body<D, 8, 1, 2, KV8>(a, t, s_kv, s_ml);
+  if (threadIdx.x == 0) s_others = 0;   // (the walk's first barrier is before any use)
+  if (t.n_rows - t.first <= 32) extend_body<D, 1, 8, 1, KV8>(a, t, s_kv, s_ml, nullptr);
+  else extend_body<D, 8, 1, 2, KV8>(a, t, s_kv, s_ml, &s_others);
 }
 
 // Folds the splits' parts: D/4 lanes a (row, query head), four outputs each, splits in order.

@@ -134,6 +134,41 @@ def test_a_query_of_nan_spoils_its_own_outputs_only():
         assert not bool(c.out.isnan().any())
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("held,new,at", [(60, 6, 57), (300, 8, 294), (500, 120, 430), (130, 130, 0), (700, 400, 301),
+                                         (260, 70, 200)])
+def test_values_of_tokens_that_a_row_does_not_see_do_not_reach_it(held, new, at, e4m3):
+    """Token `at` has an infinite (e4m3: NaN) value element and the token after it a key of NaN: rows
+    before them are as if both were not there, rows that see the value have it in that element alone, rows
+    that see the key are NaN."""
+    c = Call([held, 20], [new, 3], 8, 2, 128, e4m3=e4m3, seed=held)
+    k, v = c.kv._tensors[:2]
+    place = lambda t: (int(c.cache.table[0, t // 16]), slice(None), t % 16)   # noqa: E731
+    raw = v.view(torch.uint8 if e4m3 else torch.int16)
+    raw[place(at)][:, 5] = 0x7F if e4m3 else 0x7F80
+    if at + 1 < held:
+        k.view(raw.dtype)[place(at + 1)] = 0x7F if e4m3 else 0x7FC0
+    c.run()
+    torch.cuda.synchronize()
+    out = c.out.cpu()
+    for j in sorted({*range(0, new, max(1, new // 40)), *(x for x in (at - held + new - 1, at - held + new,
+                                                                     at - held + new + 1) if 0 <= x < new)}):
+        last = held - new + j
+        if last > at:
+            assert bool(out[j].isnan().all()), j     # it sees the key of NaN
+            continue
+        keys = c.cache.tokens(0, 0, range(last + 1))
+        values = c.cache.tokens(1, 0, range(last + 1))
+        want, tol = attend(c.q[j], keys, values, c.scale, P_ROUND)
+        got = out[j].clone()
+        if last == at:
+            assert not bool(got[:, 5].isfinite().any()), j
+            got[:, 5] = want[:, 5].to(got.dtype)
+        assert worst(got, want, tol) <= 1, j
+    want, tol = attend(c.q[new], c.cache.tokens(0, 1, range(18)), c.cache.tokens(1, 1, range(18)), c.scale, P_ROUND)
+    assert worst(out[new], want, tol) <= 1
+
+
 def test_single_tokens_without_offsets_match_the_decode_layer():
     lens = [1, 31, 500, 1024]
     c = Call(lens, [1] * 4, 8, 2, 128, seed=43, offsets=False)
