@@ -52,8 +52,9 @@ typedef struct {
  * q, k, v, q_out and the caches are 16-byte aligned (else DELTA_ERR_INVALID_ARG).  A run whose
  * sequence cannot hold it (seq_lens[b] below the run's length, or above max_pages_per_seq *
  * page_size) is skipped: nothing of it is written.  One kernel launch; no workspace.  n_rows == 0
- * does nothing.  Uses all of `shape` but max_seq_len and sm_scale.  A debug build skips tokens
- * whose page-table entry fails its check. */
+ * does nothing; 2^24 rows or more, or more than 2^28 query heads in all, give
+ * DELTA_ERR_UNSUPPORTED.  Uses all of `shape` but max_seq_len and sm_scale.  A debug build skips
+ * tokens whose page-table entry fails its check. */
 int delta_rope_append(const delta_shape_t* shape, const delta_kv_t* kv, const delta_rope_t* rope,
                       int32_t n_rows, const int32_t* row_offsets, const void* q,
                       int64_t q_row_stride, const void* k, int64_t k_row_stride, const void* v,

@@ -119,6 +119,7 @@ int delta_rope_append(const delta_shape_t* shape, const delta_kv_t* kv, const de
   if (rc) return rc;
   if ((rc = check_kv(kv))) return rc;
   if ((rc = check_runs(shape, n_rows, row_offsets))) return rc;
+  if (n_rows >= 1 << 24) return DELTA_ERR_UNSUPPORTED;   // (a launch has fewer than 2^32 threads)
   if (rope) {
     if (!rope->inv_freq || rope->rotary_dim < 16 || rope->rotary_dim > shape->head_dim ||
         rope->rotary_dim % 16 || (rope->interleaved != 0 && rope->interleaved != 1))

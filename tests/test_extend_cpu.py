@@ -49,6 +49,11 @@ def test_append_arguments(kw, rc):
     assert append(**kw) == rc
 
 
+def test_append_refuses_more_rows_than_a_launch_has_workgroups():
+    small = shape(batch=1, n_q_heads=1, n_kv_heads=1, head_dim=64)
+    assert append(small, n_rows=1 << 24, qs=64, ks=64, vs=64) == -2
+
+
 def extend(s=None, n_rows=4, max_new=1, offsets=FAKE, q=FAKE, out=FAKE, ws=FAKE, ws_bytes=1 << 40):
     kv = D.delta_kv_t(0x1000, 0x1000, 0x1000, 0x1000, 0)
     return D._lib.delta_extend_attn(ctypes.byref(s or shape()), ctypes.byref(kv), n_rows, max_new, offsets, q, out,
