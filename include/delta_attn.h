@@ -88,7 +88,8 @@ typedef struct {
 /* What a KV cache holds: bf16, or the 8-bit float e4m3 (OCP FP8: 4 exponent and 3 mantissa bits,
  * largest finite value 448, no infinity).  An e4m3 value stands for itself times the scale of its
  * KV head: key = k * k_scale[h], value = v * v_scale[h].  Half the bytes of every layer, at a
- * relative rounding of at most 2^-4 per value. */
+ * relative rounding of at most 2^-4 per value.  e4m3 caches are 16-byte aligned (else
+ * DELTA_ERR_INVALID_ARG). */
 enum { DELTA_KV_BF16 = 0, DELTA_KV_E4M3 = 1 };
 
 /* One layer's paged KV cache (Sec. 4 "Page-based DELTA"; never evicted, Sec. 4).  The layers of a

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <math.h>
+#include <stdint.h>
 
 #include "../../include/delta_attn.h"
 #include "internal.h"
@@ -35,6 +36,10 @@ inline int check_kv(const delta_kv_t* kv) {
   if (kv->kv_type != DELTA_KV_BF16 && kv->kv_type != DELTA_KV_E4M3) return DELTA_ERR_INVALID_ARG;
   // (scales of a bf16 cache would be ignored: refused instead)
   if (kv->kv_type == DELTA_KV_BF16 && (kv->k_scale || kv->v_scale)) return DELTA_ERR_INVALID_ARG;
+  // (bytes may start anywhere; the kernels load 16 of them at a time)
+  if (kv->kv_type == DELTA_KV_E4M3 &&
+      (reinterpret_cast<uintptr_t>(kv->k_cache) | reinterpret_cast<uintptr_t>(kv->v_cache)) % 16)
+    return DELTA_ERR_INVALID_ARG;
   return DELTA_OK;
 }
 
