@@ -62,7 +62,10 @@ int delta_rope_append(const delta_shape_t* shape, const delta_kv_t* kv, const de
 
 /* Bytes of workspace that are enough for delta_extend_attn with this shape, for every call of at
  * most n_rows rows and runs of at most max_new (host only): 4 (head_dim + 3) bytes and a little per
- * part of an output, of which a call keeps at most 32 per row and query head and 131072 in all. */
+ * part of an output, of which a call keeps at most 32 per row and query head and 131072 in all.
+ * Calls of more than 65535 tiles give DELTA_ERR_UNSUPPORTED here and in delta_extend_attn: the fewer
+ * of batch * ceil(max_new * G / 256) and n_rows * G / 256 + min(batch, n_rows), G query heads per KV
+ * head (up to two million rows at G = 8, more at smaller G or in batches of short runs). */
 int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int32_t max_new,
                                  size_t* out);
 

@@ -13,6 +13,8 @@ namespace delta {
 // keeps (68 MB at head size 128): with the second a call's workspace grows with its rows and nothing
 // else, so that one sized for the most rows serves every smaller call.
 constexpr int kMostSplits = 32, kMostParts = 1 << 17;
+// Most tiles of a call: a launch's second grid size.
+constexpr int kMostTiles = 65535;
 
 // Which kernel, and into how many pieces the keys are cut.  The host knows no run but the longest, so
 // it takes the rows for runs of that length and single tokens.
@@ -44,13 +46,19 @@ ExtendPlan plan_extend(const delta_shape_t* s, int n_rows, int max_new) {
     return Cut{keys / keys_per_unit / splits * std::max(1.0, wgs * splits / kCus), splits};
   };
   const Cut few = cut(32, 1.0, 128), many = cut(256, 0.25, 32);
-  const bool is_few = (int64_t)max_new * G <= 32 || few.cost <= many.cost + kStart;
+  // the grid: every run ends in a partial tile, so at most one tile per run more than whole ones
+  auto tiles_of = [&](int rows) {
+    const int64_t by_run = (int64_t)s->batch * (((int64_t)max_new * G + rows - 1) / rows);
+    const int64_t by_row = (int64_t)n_rows * G / rows + std::min(s->batch, n_rows);
+    return (int)std::min(by_run, by_row);
+  };
+  // (what the few-row kernel's smaller tiles would make too many goes to the other, whose tiles never
+  // get fewer with more rows or longer runs: a call that is taken has no smaller one that is refused)
+  const bool is_few =
+      ((int64_t)max_new * G <= 32 || few.cost <= many.cost + kStart) && tiles_of(32) <= kMostTiles;
   ExtendPlan p;
   p.rows = is_few ? 32 : 256;
-  // the grid: every run ends in a partial tile, so at most one tile per run more than whole ones
-  const int64_t by_run = (int64_t)s->batch * (((int64_t)max_new * G + p.rows - 1) / p.rows);
-  const int64_t by_row = (int64_t)n_rows * G / p.rows + std::min(s->batch, n_rows);
-  p.tiles = (int)std::min(by_run, by_row);
+  p.tiles = tiles_of(p.rows);
   const int n = is_few ? few.splits : many.splits;
   p.split_keys = ceil_div(ceil_div(s->max_seq_len, n), kFewestKeys) * kFewestKeys;
   p.n_split = ceil_div(s->max_seq_len, p.split_keys);
@@ -99,7 +107,7 @@ int extend_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, Exten
   if ((int64_t)n_rows * s->n_q_heads > (1 << 28)) return DELTA_ERR_UNSUPPORTED;
   L->n_rows = (int)std::min<int64_t>(n_rows, (int64_t)s->batch * max_new);
   L->plan = plan_extend(s, L->n_rows, max_new);
-  if (L->plan.tiles > 65535) return DELTA_ERR_UNSUPPORTED;
+  if (L->plan.tiles > kMostTiles) return DELTA_ERR_UNSUPPORTED;
   const size_t rows = (size_t)L->n_rows * s->n_q_heads;
   if (L->plan.n_split > 1) L->total = lay_out(rows, L->plan.n_split * rows, s->head_dim, L);
   else L->total = lay_out(0, 0, s->head_dim, L);

@@ -88,3 +88,23 @@ def test_workspace_grows_with_the_rows_alone():
                                   ws_bytes=E.delta_extend_workspace_bytes(s, n, m)) == -1
     with pytest.raises(D.DeltaError):
         E.delta_extend_workspace_bytes(shape(n_kv_heads=1, n_q_heads=16), 1, 1)
+
+
+@pytest.mark.parametrize("batch,held,larger,smaller", [(16384, 128, (327680, 20), (262144, 16)),
+                                                       (20000, 64, (640000, 32), (320000, 16))])
+def test_a_call_smaller_than_one_that_is_taken_is_taken(batch, held, larger, smaller):
+    """More than 65535 tiles of 32 rows: the call goes to the kernel of larger tiles."""
+    s = shape(batch=batch, n_q_heads=8, n_kv_heads=1, max_pages_per_seq=-(-held // 16), max_seq_len=held)
+    size = E.delta_extend_workspace_bytes(s, *larger)
+    assert E.delta_extend_workspace_bytes(s, *smaller) <= size
+    for n_rows, max_new in (larger, smaller):
+        assert extend(s=s, n_rows=n_rows, max_new=max_new, q=None, ws_bytes=size) == -1   # (null queries)
+
+
+def test_more_tiles_than_a_launch_has_are_refused():
+    """2^21 rows of 8 query heads per KV head are 65536 tiles of 256 rows."""
+    s = shape(batch=1, n_q_heads=8, n_kv_heads=1, max_pages_per_seq=1 << 17, max_seq_len=1 << 21)
+    assert extend(s=s, n_rows=1 << 21, max_new=1 << 21, q=None) == -2
+    assert extend(s=s, n_rows=(1 << 21) - 512, max_new=(1 << 21) - 512, q=None) == -1
+    with pytest.raises(D.DeltaError):
+        E.delta_extend_workspace_bytes(s, 1 << 21, 1 << 21)
