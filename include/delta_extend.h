@@ -65,7 +65,8 @@ int delta_rope_append(const delta_shape_t* shape, const delta_kv_t* kv, const de
  * part of an output, of which a call keeps at most 32 per row and query head and 131072 in all.
  * Calls of more than 65535 tiles give DELTA_ERR_UNSUPPORTED here and in delta_extend_attn: the fewer
  * of batch * ceil(max_new * G / 256) and n_rows * G / 256 + min(batch, n_rows), G query heads per KV
- * head (up to two million rows at G = 8, more at smaller G or in batches of short runs). */
+ * head (up to two million rows at G = 8, more at smaller G or in batches of short runs).  So do
+ * shapes whose max_seq_len is above 2^31 - 512. */
 int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int32_t max_new,
                                  size_t* out);
 

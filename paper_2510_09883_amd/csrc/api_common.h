@@ -12,7 +12,7 @@ namespace delta {
 constexpr size_t kAlign = 256;
 
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+inline int ceil_div(int a, int b) { return (int)(((int64_t)a + b - 1) / b); }
 
 inline int check_shape(const delta_shape_t* s) {
   if (!s) return DELTA_ERR_INVALID_ARG;

@@ -15,6 +15,9 @@ namespace delta {
 constexpr int kMostSplits = 32, kMostParts = 1 << 17;
 // Most tiles of a call: a launch's second grid size.
 constexpr int kMostTiles = 65535;
+// The longest bound of a sequence: the kernels round key indices up to whole blocks, of 256 keys at
+// most, in 32 bits.
+constexpr int kMostKeys = INT32_MAX - 511;
 
 // Which kernel, and into how many pieces the keys are cut.  The host knows no run but the longest, so
 // it takes the rows for runs of that length and single tokens.
@@ -104,7 +107,7 @@ int extend_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, Exten
   int rc = check_shape(s);
   if (rc) return rc;
   if (n_rows < 0 || max_new < 0 || max_new > n_rows) return DELTA_ERR_INVALID_ARG;
-  if ((int64_t)n_rows * s->n_q_heads > (1 << 28)) return DELTA_ERR_UNSUPPORTED;
+  if ((int64_t)n_rows * s->n_q_heads > (1 << 28) || s->max_seq_len > kMostKeys) return DELTA_ERR_UNSUPPORTED;
   L->n_rows = (int)std::min<int64_t>(n_rows, (int64_t)s->batch * max_new);
   L->plan = plan_extend(s, L->n_rows, max_new);
   if (L->plan.tiles > kMostTiles) return DELTA_ERR_UNSUPPORTED;
