@@ -16,7 +16,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(const AppendArgs a) {
   const int b = blockIdx.y;
   const int s = a.seq_lens[b];
-  if (s < 1 || s > 16 * a.max_pages) return;   // no token slot: nothing written
+  if (s < 1 || (s - 1) >> 4 >= a.max_pages) return;   // no token slot: nothing written
   const int t = s - 1;
   const int page = a.page_table[(size_t)b * a.max_pages + (t >> 4)];
   // debug builds: a page outside the cache is not written (there is no status word to flag it)

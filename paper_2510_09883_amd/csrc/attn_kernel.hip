@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kAttnThreads, LOGITS ? 1 : 2) void attn_kernel(cons
           const int t = sel[16 * g0 + i];
           const int ph = phys ? phys[16 * g0 + i] : 0;
           if (DELTA_DEBUG && t >= s_len) debug_flag(a.status, DELTA_DEBUG_SELECTION);
-          if (t >= 0 && t < 16 * a.max_pages) {
+          if (t >= 0 && t >> 4 < a.max_pages) {
             const int page = checked_page(phys ? ph >> 4 : pt[t >> 4], a.n_pages, a.status);
             packed = page * 16 + (phys ? ph & 15 : t & 15);
           }

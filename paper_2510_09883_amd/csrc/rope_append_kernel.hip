@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeAppendA
       const int begin = run_offset(a.runs, b), end = run_offset(a.runs, b + 1);
       const int s = a.runs.seq_lens[b];
       t = s - (end - row);
-      if (s >= end - begin && s <= 16 * a.runs.max_pages) {
+      if (s >= end - begin && (s - 1) >> 4 < a.runs.max_pages) {   // (16 * max_pages may pass 32 bits)
         const int page = a.runs.page_table[(size_t)b * a.runs.max_pages + (t >> 4)];
         if (!DELTA_DEBUG || (page >= 0 && (a.n_pages == 0 || page < a.n_pages)))
           at = (int64_t)page * a.page_stride + (t & 15) * D;
