@@ -227,6 +227,9 @@ def make_kv(k_cache, v_cache, page_table, seq_lens, k_scale=None, v_scale=None) 
     scales = [(n, _dev(n, t)) for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if t is not None]
     if scales and not e4m3:
         raise ValueError(f"{scales[0][0]}: only caches of torch.float8_e4m3fn have scales")
+    for name, t in (("v_cache", v_cache), ("page_table", page_table), ("seq_lens", seq_lens), *scales):
+        if t.device != k_cache.device:
+            raise ValueError(f"{name}: on {t.device}, but k_cache is on {k_cache.device}")
     kv = delta_kv_t(k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(),
                     k_cache.shape[0], DELTA_KV_E4M3 if e4m3 else DELTA_KV_BF16, _ptr(k_scale), _ptr(v_scale))
     kv._tensors = (k_cache, v_cache, page_table, seq_lens, scales)   # checked against the shape per call
