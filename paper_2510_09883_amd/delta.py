@@ -170,18 +170,27 @@ def _check_kv(kv, shape):
                 break
         else:
             return
+    _check_cache(shape, torch.float8_e4m3fn if kv.kv_type == DELTA_KV_E4M3 else torch.bfloat16, k, v, pt, sl, scales)
+    named = (("k_cache", k), ("v_cache", v), ("page_table", pt), ("seq_lens", sl), *scales)
+    for (name, x), (_, p) in zip(named, (*kv._made, *kv._made_scales)):
+        if x.data_ptr() != p:
+            raise ValueError(f"{name}: its memory is no longer what make_kv was given")
+
+
+def _check_cache(shape, kind, k, v, pt, sl, scales=()):
     cache = (None, shape.n_kv_heads, shape.page_size, shape.head_dim)
-    kind = torch.float8_e4m3fn if kv.kv_type == DELTA_KV_E4M3 else torch.bfloat16
     _dev("k_cache", k, kind, cache)
     _dev("v_cache", v, kind, cache)
     for name, s in scales:
         _dev(name, s, torch.float32, (shape.n_kv_heads,))
     _dev("page_table", pt, torch.int32, (shape.batch, shape.max_pages_per_seq))
     _dev("seq_lens", sl, torch.int32, (shape.batch,))
-    named = (("k_cache", k), ("v_cache", v), ("page_table", pt), ("seq_lens", sl), *scales)
-    for (name, x), (_, p) in zip(named, (*kv._made, *kv._made_scales)):
-        if x.data_ptr() != p:
-            raise ValueError(f"{name}: its memory is no longer what make_kv was given")
+
+
+def _same_pages(k, v):
+    if k.dim() < 1 or v.dim() < 1 or k.shape[0] != v.shape[0]:
+        raise ValueError(f"k_cache and v_cache must hold the same number of pages "
+                         f"(got {tuple(k.shape)}, {tuple(v.shape)})")
 
 
 def _check_qo(shape, q, out):
@@ -220,9 +229,7 @@ def make_kv(k_cache, v_cache, page_table, seq_lens, k_scale=None, v_scale=None) 
     for name, t in (("k_cache", k_cache), ("v_cache", v_cache), ("page_table", page_table),
                     ("seq_lens", seq_lens)):
         _dev(name, t)
-    if k_cache.dim() < 1 or v_cache.dim() < 1 or k_cache.shape[0] != v_cache.shape[0]:
-        raise ValueError(f"k_cache and v_cache must hold the same number of pages "
-                         f"(got {tuple(k_cache.shape)}, {tuple(v_cache.shape)})")
+    _same_pages(k_cache, v_cache)
     e4m3 = k_cache.dtype == torch.float8_e4m3fn
     scales = [(n, _dev(n, t)) for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if t is not None]
     if scales and not e4m3:
@@ -372,8 +379,9 @@ def delta_decode_step_noalloc(args: StepArgs):
 
 
 def delta_kv_append(shape, k_cache, v_cache, page_table, seq_lens, k_new, v_new):
-    _dev("k_cache", k_cache, torch.bfloat16)   # (e4m3 caches: extend.delta_rope_append)
-    _check_kv(make_kv(k_cache, v_cache, page_table, seq_lens), shape)
+    # (bf16 caches; e4m3 ones: extend.delta_rope_append)
+    _check_cache(shape, torch.bfloat16, k_cache, v_cache, page_table, seq_lens)
+    _same_pages(k_cache, v_cache)
     row = (shape.batch, shape.n_kv_heads, shape.head_dim)
     _dev("k_new", k_new, torch.bfloat16, row)
     _dev("v_new", v_new, torch.bfloat16, row)
