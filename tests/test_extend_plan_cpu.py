@@ -6,6 +6,7 @@ import shutil
 import pytest
 
 import extend_plan as P
+import many_row_cases as C
 from paper_2510_09883_amd import delta as D
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
@@ -54,3 +55,14 @@ def test_bounds_past_the_kernels_arithmetic_are_refused():
         size = ctypes.c_size_t(0)
         taken = D._lib.delta_extend_workspace_bytes(ctypes.byref(s), 4, 4, ctypes.byref(size)) == D.DELTA_OK
         assert taken == (held <= LONGEST)
+
+
+def test_the_cases_of_many_rows_go_to_that_kernel(exe):
+    """tests/test_gpu_extend_many_rows.py tests the kernel of 256-row tiles: its calls have to reach it,
+    with one piece of the keys and with several, whatever becomes of the rule."""
+    cases = [C.plan_call(*c, d) for c in (*C.MANY_ROWS, C.HIDDEN) for d in (64, 128)]
+    batch, held, new, hq, hkv = C.MOST_TILES
+    cases += [(batch, hq, hkv, 64, held, batch * new, new), (2, 10, 2, 128, 1800, 1502, 1450)]
+    plans = P.ask(exe, cases)
+    assert [p.rows for p in plans] == [256] * len(cases), [c for c, p in zip(cases, plans) if p.rows != 256]
+    assert {p.n_split > 1 for p in plans} == {False, True}
