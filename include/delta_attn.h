@@ -11,6 +11,9 @@
  *   SPARSE decode attention restricted to the selected pages (App. A, Alg. 1).
  *
  * Conventions shared by every entry point
+ *   Structs.  As this header lays them out, with neither size nor version in them: a caller is
+ *             compiled with the header of the library that it runs with.  (delta_kv_t ended with
+ *             n_pages before there were e4m3 caches.)
  *   Memory.   Structs, the `roles` array and the per-layer pointer arrays of delta_decode_step
  *             are HOST memory.  Every other pointer is DEVICE memory owned by the caller.  The
  *             library never allocates, frees, keeps a pointer, or synchronises `stream`

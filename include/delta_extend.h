@@ -7,7 +7,7 @@
  *
  * Runs.  A call covers n_rows rows, one per new token, of all sequences one after another: the
  * run of sequence b is rows row_offsets[b] .. row_offsets[b+1]-1 (int32 [batch+1], device memory,
- * not decreasing, from 0 on and at most n_rows; a run may be empty).  row_offsets == NULL: one
+ * the first 0, not decreasing, at most n_rows; a run may be empty).  row_offsets == NULL: one
  * new token per sequence, row b that of sequence b (n_rows == batch).  seq_lens[b] counts the new
  * tokens, so row j of a run of n is token seq_lens[b] - n + j of its sequence.  Rows of no run
  * (behind the last one) are neither read nor written.
@@ -76,18 +76,23 @@ int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int
  * The new tokens' keys and values stand in the cache already (delta_rope_append).
  *   q, out:  bf16 [n_rows, n_q_heads, head_dim], 16-byte aligned
  *   max_new: at least the longest run (sizes the grid; with a longer run some rows' outputs are
- *            undefined)
+ *            undefined) and at most n_rows (else DELTA_ERR_INVALID_ARG)
  *   ws:      at least delta_extend_workspace_bytes() bytes, 256-byte aligned, of any content;
  *            it keeps nothing between calls.  Calls that share one must not run concurrently.
  *            (A debug build's status word is its first: zero it before the call to read it.)
  * seq_lens[b] may be 0 (with an empty run) and is cut to max_seq_len.
+ * max_seq_len decides the speed of calls of few rows, never their results: a sequence's tokens are
+ * cut into pieces for workgroups of their own by this bound, not by seq_lens.  Where it is 8 to 32
+ * times the lengths such a call takes up to 2.7 times as long (one sequence of 4096 tokens, 8 new,
+ * 32/8 heads: 16 us with that bound, 45 with 131072); calls that fill the GPU without pieces, as long
+ * prompts do, take the same time.
  * What a row does not see does not reach it, infinite and NaN keys and values of later tokens and of
  * rows past the sequence among it; those that it sees can make its outputs infinite or NaN (a value
  * its own element, a key all), and a NaN query its own outputs.
- * bf16 queries, fp32 scores, softmax and sums, one bf16 rounding of the result; where a kernel
- * works on whole tiles of rows (see max_new) the probabilities are rounded to bf16 before they
- * meet the values (at most 2^-8 of each), their sum is not.  Deterministic: the same call
- * gives the same bits. */
+ * bf16 queries, fp32 scores, softmax and sums, one bf16 rounding of the result; the probabilities
+ * are rounded to bf16 before they meet the values (at most 2^-8 of each), their sum is not.  (The
+ * decode step's attention of a single token keeps them in three bf16 terms.)  Deterministic: the
+ * same call gives the same bits. */
 int delta_extend_attn(const delta_shape_t* shape, const delta_kv_t* kv, int32_t n_rows,
                       int32_t max_new, const int32_t* row_offsets, const void* q, void* out,
                       void* ws, size_t ws_bytes, void* stream);

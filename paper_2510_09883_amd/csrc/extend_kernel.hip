@@ -37,8 +37,12 @@
 //
 // Precision.  Scores, maximum, sum and outputs are fp32; a probability is rounded to bf16 for the
 // P V product, whose inputs the matrix cores take in 16 bits: at most 2^-8 of each, which in the
-// output adds to the result's own rounding (1.7e-3 rms together instead of 1.6e-3).  Three bf16 terms
-// per probability, as the decode kernel has them for free in idle columns, would double the products.
+// output adds to the result's own rounding (1.7e-3 rms together instead of 1.6e-3, 1.8e-3 where rows see
+// a few tokens only).  A second bf16 term per probability, what the first leaves, needs half as many
+// products again, of which the many-row kernel has 356 us in the prompt below.  Runs of at most 32 rows,
+// which wait for memory, pay for it too, us without and with it, 32/8 heads: 16 sequences of 16384
+// tokens, 8 new ones 170 and 172 (e4m3 110 and 124), 8 of 4096, 4 new ones 27.8 and 29.9, 16 of 300, 8
+// new ones 9.8 and 10.7.
 //
 // Bound.  Many rows: the card's power, then the issue of two waves a SIMD.  A prompt of 8192 tokens,
 // 32/8 heads: 580-640 us from card to card (860-950 TFLOP/s, where the library's product of 8192 x 8192
