@@ -48,7 +48,7 @@ typedef struct {
  *          values only.  k, v: the same with n_kv_heads.  q, k and v may be views of one
  *          projection's output.
  *   q_out: bf16 [n_rows, n_q_heads, head_dim]; may be q itself where q's rows lie one behind the
- *          other, and must not overlap the inputs otherwise.
+ *          other (else DELTA_ERR_INVALID_ARG), and must not overlap the inputs otherwise.
  * q, k, v, q_out and the caches are 16-byte aligned (else DELTA_ERR_INVALID_ARG).  A run whose
  * sequence cannot hold it (seq_lens[b] below the run's length, or above max_pages_per_seq *
  * page_size) is skipped: nothing of it is written.  One kernel launch; no workspace.  n_rows == 0

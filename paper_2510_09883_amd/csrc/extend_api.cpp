@@ -143,6 +143,8 @@ int delta_rope_append(const delta_shape_t* shape, const delta_kv_t* kv, const de
   if (k_row_stride < kv_row || k_row_stride % 8 || v_row_stride < kv_row || v_row_stride % 8 ||
       (q && (q_row_stride < q_row || q_row_stride % 8)))
     return DELTA_ERR_INVALID_ARG;
+  // (in place, rows that stand apart would be written over rows still to be read)
+  if (q && q == q_out && q_row_stride != q_row && n_rows > 1) return DELTA_ERR_INVALID_ARG;
   for (const void* p : {q, k, v, static_cast<const void*>(q_out), kv->k_cache, kv->v_cache})
     if (!aligned(p, 16)) return DELTA_ERR_INVALID_ARG;
   RopeAppendArgs a{};

@@ -108,3 +108,8 @@ def test_more_tiles_than_a_launch_has_are_refused():
     assert extend(s=s, n_rows=(1 << 21) - 512, max_new=(1 << 21) - 512, q=None) == -1
     with pytest.raises(D.DeltaError):
         E.delta_extend_workspace_bytes(s, 1 << 21, 1 << 21)
+
+
+def test_rotation_in_place_of_rows_that_stand_apart_is_refused():
+    """q_out's rows lie one behind the other: over such a q they would fall on rows still to be read."""
+    assert append(qs=1536) == -1
