@@ -82,7 +82,7 @@ int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int
  *            (A debug build's status word is its first: zero it before the call to read it.)
  * seq_lens[b] may be 0 (with an empty run) and is cut to max_seq_len.
  * max_seq_len decides the speed of calls of few rows, never their results: a sequence's tokens are
- * cut into pieces for workgroups of their own by this bound, not by seq_lens.  Where it is 8 to 32
+ * cut into pieces for workgroups of their own by this bound, not by seq_lens.  Where it is 4 to 32
  * times the lengths such a call takes up to 2.7 times as long (one sequence of 4096 tokens, 8 new,
  * 32/8 heads: 16 us with that bound, 45 with 131072); calls that fill the GPU without pieces, as long
  * prompts do, take the same time.
