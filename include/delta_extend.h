@@ -83,9 +83,9 @@ int delta_extend_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int
  * seq_lens[b] may be 0 (with an empty run) and is cut to max_seq_len.
  * max_seq_len decides the speed of calls of few rows, never their results: a sequence's tokens are
  * cut into pieces for workgroups of their own by this bound, not by seq_lens.  Where it is 4 to 32
- * times the lengths such a call takes up to 2.7 times as long (one sequence of 4096 tokens, 8 new,
- * 32/8 heads: 16 us with that bound, 45 with 131072); calls that fill the GPU without pieces, as long
- * prompts do, take the same time.
+ * times the lengths such a call takes up to 2.7 times as long (32/8 heads, one sequence of 4096
+ * tokens, 8 new: 16 us with a bound of 4096, 45 with 131072; 512 new behind 7680: 94 with 8192, 240
+ * with 32768).  Calls that fill the GPU without pieces, as long prompts do, take the same time.
  * What a row does not see does not reach it, infinite and NaN keys and values of later tokens and of
  * rows past the sequence among it; those that it sees can make its outputs infinite or NaN (a value
  * its own element, a key all), and a NaN query its own outputs.
