@@ -115,7 +115,7 @@ def draw(rng):
             if rows * c["vocab"] * (8 if c["drafted"] else 4) > _MOST_BYTES:
                 continue
         else:
-            c["layers"] = rng.choice([1, 2, 28, 32, 48])
+            c["layers"] = rng.choice([1, 2, 28])
             c["new_lo"] = max(1, c["new_lo"])
             c["new_hi"] = max(c["new_hi"], c["new_lo"])
             if c["batch"] * c["hi"] * token * c["layers"] > _MOST_BYTES:
