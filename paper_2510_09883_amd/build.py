@@ -20,6 +20,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["attn_kernel.hip", "fused_delta_kernel.hip", "select_kernel.hip", "append_kernel.hip",
            "rope_append_kernel.hip", "extend_kernel.hip", "extend_api.cpp",
+           "tree_layout_kernel.hip", "tree_attn_kernel.hip", "verify_kernel.hip", "compact_kernel.hip",
+           "drafts_api.cpp",
            "probe_kernel.hip", "noalloc.hip", "delta_api.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-mcode-object-version=5",

@@ -1,0 +1,78 @@
+// Internal interface between drafts_api.cpp and the kernels for a round of drafted tokens
+// (tree_layout_kernel.hip, tree_attn_kernel.hip, verify_kernel.hip, compact_kernel.hip).
+#pragma once
+
+#include "../../include/delta_drafts.h"
+#include "extend.h"
+
+namespace delta {
+
+constexpr int kMostDrafts = DELTA_MOST_DRAFTS;
+
+struct TreeLayoutArgs {
+  Runs runs;                 // (page_table unused; seq_lens may be null without positions)
+  const int32_t* parents;    // [n_rows]
+  int32_t* positions;        // [n_rows] or null
+  uint32_t* masks;           // [n_rows, mask_words] or null
+  int32_t mask_words, max_new;
+};
+
+hipError_t launch_tree_layout(const TreeLayoutArgs& a, hipStream_t stream);
+
+ExtendPlan plan_tree(const delta_shape_t* s, int n_rows, int max_new);
+hipError_t launch_tree_attn(const ExtendPlan& p, int head_dim, bool kv8, const ExtendArgs& a, hipStream_t stream);
+
+// Pieces of a row of probabilities, each summed by a workgroup of its own.
+constexpr int kMostPieces = 64, kMostPiece = 16384;   // and their elements
+constexpr int kMostVocab = kMostPieces * kMostPiece;
+
+// A sequence's part of the workspace: at a place that does not depend on the batch, so that calls of any size
+// leave the counters of all zero.
+struct VerifyState {
+  int32_t arrived;           // workgroups that are done; zero between launches
+  int32_t pad[kCounterStride - 1];
+  double sums[kMostPieces][2];   // a piece's sums of r and of p
+};
+
+struct VerifyArgs {
+  Runs runs;                 // (only the offsets; n_rows, batch)
+  const float* target;       // rows target_stride elements apart
+  const float* draft;        // or null
+  int64_t target_stride, draft_stride;
+  const int32_t* tokens;     // [n_rows]
+  const int32_t* parents;
+  const float* uniform;
+  int32_t* path;             // [batch, max_new]
+  int32_t* n_path;           // [batch]
+  int32_t* next;             // [batch]
+  VerifyState* state;        // [batch]
+  int32_t vocab, max_new;
+  int32_t n_pieces;          // workgroups per sequence
+};
+
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream);
+
+// Layers of one launch of the compaction (their pointers are kernel arguments).
+constexpr int kLayersPerLaunch = 64;
+
+struct CompactLayer {
+  uint8_t* k_cache;          // [pages, Hkv, 16, D], 1 or 2 bytes an element
+  uint8_t* v_cache;
+  const int32_t* page_table; // [B, max_pages]
+  int64_t n_pages;           // 0: not stated; debug checks
+};
+
+struct CompactArgs {
+  Runs runs;                 // (page_table unused)
+  const int32_t* path;       // [batch, max_new]
+  const int32_t* n_path;     // [batch]
+  int32_t* new_lens;         // [batch] or null
+  int32_t max_new, n_kv_heads, head_dim, n_layers;
+  uint64_t e4m3;             // bit i: layer i's caches have 1 byte an element
+  CompactLayer layers[kLayersPerLaunch];
+};
+
+hipError_t launch_compact(const CompactArgs& a, hipStream_t stream);
+hipError_t launch_compact_lens(const CompactArgs& a, hipStream_t stream);
+
+}  // namespace delta

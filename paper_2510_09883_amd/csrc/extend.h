@@ -37,6 +37,17 @@ struct RopeAppendArgs {
 
 hipError_t launch_rope_append(int head_dim, bool kv8, const RopeAppendArgs& a, hipStream_t stream);
 
+// Norms of the queries' and keys' heads, taken before they turn.
+struct HeadNorm {
+  const void* q_weight;      // [head_dim], bf16 or fp32 (f32); null: 1
+  const void* k_weight;
+  bool f32;
+  float eps;
+};
+
+hipError_t launch_norm_rope_append(int head_dim, bool kv8, const RopeAppendArgs& a, const HeadNorm& norm,
+                                   hipStream_t stream);
+
 struct ExtendArgs {
   Runs runs;
   const uint8_t* k_cache;
@@ -56,6 +67,8 @@ struct ExtendArgs {
   float scale_log2;
   int64_t n_pages;
   uint32_t* status;          // debug status word
+  const uint32_t* masks;     // [n_rows, mask_words] rows of its run that a row sees (trees only)
+  int32_t mask_words;
 };
 
 // How a call is cut: tiles of `rows` (token, query head of the group) rows per (sequence, KV

@@ -5,6 +5,9 @@
 // The angle p f of a far position has an fp32 rounding error of 2^-24 p f (0.008 radians at 131072),
 // so it is formed in fp64 and reduced there to [-pi, pi] before the fp32 sine and cosine.
 //
+// With a norm (rope_append_kernel<.., NORM>) a head's queries or keys x become w x / sqrt(mean(x^2) + eps)
+// before they turn: the lanes that hold a head sum its squares among themselves, in registers.
+//
 // Work.  A workgroup takes `tokens` rows (see launch_rope_append).  Wave w finds row w's sequence,
 // position and place in the cache, and its lanes the cosines and sines of the row's at most 64
 // angles, once for all heads, into LDS.  Then every thread takes units of 16 head elements: two
@@ -63,8 +66,32 @@ __device__ __forceinline__ u32x2 pack_e4m3(const float (&x)[8], float scale) {
   return w;
 }
 
-template <int D, bool KV8>
-__global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeAppendArgs a, int tokens) {
+// Sum over the UPH neighbouring lanes that hold a head (4 or 8), in all of them; each lane of a pair adds
+// the same two numbers, so all get the same bits.
+template <int UPH>
+__device__ __forceinline__ float head_sum(float x) {
+  x += lane_xor1(x);
+  x += lane_xor2(x);
+  // (quads hold one value now: the mirrored half row is the other quad)
+  if (UPH == 8) x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x141, 0xf, 0xf, false));
+  return x;
+}
+
+// Eight norm weights from element e on (null: 1).
+__device__ __forceinline__ void norm_weights(const void* w, bool f32, int e, float (&x)[8]) {
+  if (!w) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = 1.f;
+  } else if (f32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = static_cast<const float*>(w)[e + i];
+  } else {
+    unpack8(*reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(w) + e), x);
+  }
+}
+
+template <int D, bool KV8, bool NORM>
+__global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeAppendArgs a, const HeadNorm norm, int tokens) {
   constexpr int UPH = D / 16;   // units per head
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -120,6 +147,23 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeAppendA
     float x[8], y[8];
     unpack8(*reinterpret_cast<const u32x4*>(src + e0), x);
     unpack8(*reinterpret_cast<const u32x4*>(src + e1), y);
+    if (NORM && !is_v) {
+      // fp32 throughout, one rounding at the end: the square mean, its root's inverse, times the weight
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += x[j] * x[j] + y[j] * y[j];
+      sum = head_sum<UPH>(sum);
+      const float inv = 1.f / sqrtf(sum * (1.f / D) + norm.eps);
+      float wx[8], wy[8];
+      const void* w = is_q ? norm.q_weight : norm.k_weight;
+      norm_weights(w, norm.f32, e0, wx);
+      norm_weights(w, norm.f32, e1, wy);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[j] = x[j] * inv * wx[j];
+        y[j] = y[j] * inv * wy[j];
+      }
+    }
     if (turn) {
       float2 cs[8];
 #pragma unroll
@@ -164,9 +208,8 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeAppendA
   }
 }
 
-}  // namespace
-
-hipError_t launch_rope_append(int head_dim, bool kv8, const RopeAppendArgs& a, hipStream_t stream) {
+template <bool NORM>
+hipError_t launch(int head_dim, bool kv8, const RopeAppendArgs& a, const HeadNorm& norm, hipStream_t stream) {
   // One row a workgroup: rows are then looked up and their angles formed in parallel.  Several share
   // one only where a row leaves most of the threads idle and there are rows enough to fill the device.
   // Measured on MI355X, us, one and four rows a workgroup: 64 rows of 32/8 heads 3.9 and 6.2, 1024 6.1
@@ -177,13 +220,24 @@ hipError_t launch_rope_append(int head_dim, bool kv8, const RopeAppendArgs& a, h
   const int tokens = units <= kThreads / 2 && a.runs.n_rows >= 4096 ? kMaxTokens : 1;
   const dim3 grid((a.runs.n_rows + tokens - 1) / tokens), block(kThreads);
   if (head_dim == 128) {
-    if (kv8) hipLaunchKernelGGL((rope_append_kernel<128, true>), grid, block, 0, stream, a, tokens);
-    else hipLaunchKernelGGL((rope_append_kernel<128, false>), grid, block, 0, stream, a, tokens);
+    if (kv8) hipLaunchKernelGGL((rope_append_kernel<128, true, NORM>), grid, block, 0, stream, a, norm, tokens);
+    else hipLaunchKernelGGL((rope_append_kernel<128, false, NORM>), grid, block, 0, stream, a, norm, tokens);
   } else {
-    if (kv8) hipLaunchKernelGGL((rope_append_kernel<64, true>), grid, block, 0, stream, a, tokens);
-    else hipLaunchKernelGGL((rope_append_kernel<64, false>), grid, block, 0, stream, a, tokens);
+    if (kv8) hipLaunchKernelGGL((rope_append_kernel<64, true, NORM>), grid, block, 0, stream, a, norm, tokens);
+    else hipLaunchKernelGGL((rope_append_kernel<64, false, NORM>), grid, block, 0, stream, a, norm, tokens);
   }
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rope_append(int head_dim, bool kv8, const RopeAppendArgs& a, hipStream_t stream) {
+  return launch<false>(head_dim, kv8, a, HeadNorm{}, stream);
+}
+
+hipError_t launch_norm_rope_append(int head_dim, bool kv8, const RopeAppendArgs& a, const HeadNorm& norm,
+                                   hipStream_t stream) {
+  return launch<true>(head_dim, kv8, a, norm, stream);
 }
 
 }  // namespace delta
