@@ -98,17 +98,78 @@ struct TileOf {
   int s_b;       // tokens of the sequence
 };
 
+// What of a tile's keys a workgroup takes, and where its outputs go.
+struct Piece {
+  int g;              // KV head
+  int blk0, blk1;     // blocks of keys (32 * KT * WK of them)
+  bool whole;         // all that the tile sees: the result is written
+  int note;           // what part_n gets for every row; -1: nothing.  (TREE: with the row's place in the tile from
+                      // bit 20 on, except for 0)
+  size_t part;        // the part: index of row 0 (TREE: of the tile; else of the call)
+};
+
+// The arguments of a kernel whose only parameter they are, read anew.  Kept from the kernel's start they take the
+// scalar registers that the products' schedule needs (without them it waits for LDS before every product).
+__device__ __forceinline__ ExtendArgs read_args() {
+  typedef const __attribute__((address_space(4))) uint64_t* Kernarg;
+  static_assert(sizeof(ExtendArgs) % 8 == 0, "whole words");
+  struct Words {
+    uint64_t w[sizeof(ExtendArgs) / 8];
+  } words;
+  Kernarg kernarg = (Kernarg)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(kernarg));
+#pragma unroll
+  for (size_t i = 0; i < sizeof(ExtendArgs) / 8; ++i) words.w[i] = kernarg[i];
+  return __builtin_bit_cast(ExtendArgs, words);
+}
+
+// A value that is the same in all lanes, in a vector register.
+__device__ __forceinline__ int held(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Words of a row's mask at most, and tokens of a tile: their masks stand in LDS.
+constexpr int kMostMaskWords = 16;
+template <int ROWS>
+constexpr int kMaskLds = (ROWS + 2) * kMostMaskWords;
+
+// Blocks that a ring holds, and the pages that it looks up at a time.
+constexpr int kRing = 4, kRingPages = 1024;
+
 // LDS of a body, in bytes: K and V of the blocks, later the outputs of the waves along the keys.
-template <int D, int WR, int WK, int KT>
-constexpr int kBodyLds = std::max(2 * (WR == 1 ? 1 : 2) * 32 * KT * WK * D * 2, WK > 1 ? WK * 64 * D / 2 * 4 : 0);
+template <int D, int WR, int WK, int KT, bool RING = false, bool KV8 = false>
+constexpr int kBodyLds = std::max(RING ? (KV8 ? 2 * 2 * 2 + kRing * 2 : kRing * 2 * 2) * 32 * KT * WK * D
+                                       : 2 * (WR == 1 ? 1 : 2) * 32 * KT * WK * D * 2,
+                                  WK > 1 ? WR * WK * 64 * D / 2 * 4 : 0);
+
+// Loads 16 bytes a lane to LDS, lane after lane from byte `lds` on, past the registers.  Nothing but load_wait waits
+// for it.
+__device__ __forceinline__ void load_to_lds(const uint8_t* from, uint32_t lds) {
+  uint32_t m0;   // (kept: the compiler takes it for its own)
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off nt\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(lds), "v"(from)
+               : "memory");
+}
+// All but the last N loads of the wave are done.  (Loads that the compiler knows of count too: then it waits longer.)
+template <int N>
+__device__ __forceinline__ void load_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
 // What a row sees.  Causal runs: the tokens up to itself.  TREE: the tokens before the run, and of the
 // run's rows those whose bits are set in the row's mask.
-template <int D, int WR, int WK, int KT, bool KV8, bool TREE>
-__device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t, uint16_t* s_kv, float2* s_ml,
-                                            int* s_others) {
+//
+// RING: the blocks are brought by loads that go to LDS, kRing - 1 of them under way while one is worked on; bf16
+// blocks where the products read them, e4m3 ones to LDS of the wave that loads them, which makes bf16 of them
+// (the two buffers of the other forms) one block ahead.
+template <int D, int WR, int WK, int KT, bool KV8, bool TREE, bool RING = false>
+__device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t, const Piece& piece,
+                                            uint16_t* s_kv, float2* s_ml, int* s_others, int* s_pages = nullptr,
+                                            uint32_t* s_masks = nullptr) {
+  static_assert(!RING || WR > 1, "waves that share blocks");
   constexpr int NW = WR * WK, T = 64 * NW;
-  constexpr int BM = 32 * WR;           // rows of a tile
   constexpr int BK = 32 * KT;           // keys a wave takes of a block
   constexpr int BN = BK * WK;           // keys of a block
   constexpr int NK = D / 16;            // MFMA steps of a score tile
@@ -119,11 +180,15 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   constexpr int NL = (kPieces + T - 1) / T;   // loads per thread and block (the last waves may have none)
   constexpr int RPW = 64 / CPR;         // rows of a wave-wide load
   static_assert(kPieces % 64 == 0 && 16 % RPW == 0, "whole loads, each inside one page");
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int tid = threadIdx.x;
+  // (a workgroup takes several tiles: what follows from the lane is formed for each anew, as kept in registers
+  // from tile to tile it would not fit them)
+  if (TREE) asm volatile("" : "+v"(tid));
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % WR, wk = wave / WR;
   const int n = lane & 31, h = lane >> 5;
-  const int g = blockIdx.x, split = blockIdx.z;
+  const int g = piece.g;
   const int Hq = a.n_q_heads, G = Hq / a.n_kv_heads;
 
   // Waves that share no rows share no keys either: each brings its own keys to its own LDS, without
@@ -144,31 +209,46 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   auto lim_of = [&](int row) { return max(0, base + min(row, n_tile_rows - 1) / G + 1); };
   // of the wave's rows: keys that all see, and that none sees
   const int lim_lo = TREE ? max(0, base) : lim_of(r0), lim_hi = TREE ? s_b : lim_of(r0 + 31);
-  // TREE: which of keys key0 .. key0 + 31 the row sees (bit 0: key0)
-  const uint32_t* mask = TREE ? a.masks + (size_t)(begin + j) * a.mask_words : nullptr;
+  // TREE: which of keys key0 .. key0 + 31 the row sees (bit 0: key0), from the masks of the tile's tokens in LDS
+  const int words = TREE ? min(kMostMaskWords, min(a.mask_words, (n_new + 31) / 32)) : 0;
+  const int j0 = t.first / G;
   auto mask_word = [&](int w) -> uint32_t {
-    if (w < 0) return ~0u;   // tokens before the run
-    if (w >= a.mask_words || 32 * w >= n_new) return 0u;
-    const int left = n_new - 32 * w;
-    return mask[w] & (left >= 32 ? ~0u : (1u << left) - 1u);
+    return w < 0 ? ~0u /* tokens before the run */ : w >= words ? 0u : s_masks[(j - j0) * words + w];
   };
   auto seen_of = [&](int key0) -> uint32_t {
     const int w = (key0 - base) >> 5, shift = (key0 - base) & 31;
     return __builtin_amdgcn_alignbit(mask_word(w + 1), mask_word(w), shift);
   };
 
-  const int n_blocks = ((TREE ? s_b : lim_of(t.first + BM - 1)) + BN - 1) / BN;
-  // pieces of one length whatever the sequence's: a short sequence has fewer
-  const int per_split = a.split_keys / BN;
-  const int n_valid = max(1, (n_blocks + per_split - 1) / per_split);
-  if (split >= n_valid) return;
-  const int blk0 = split * per_split, blk1 = min(n_blocks, blk0 + per_split);
+  const int blk0 = piece.blk0, blk1 = piece.blk1;
 
   const float scale = KV8 && a.k_scale ? a.scale_log2 * a.k_scale[g] : a.scale_log2;
   bf16x8 q[NK];
 #pragma unroll
   for (int ks = 0; ks < NK; ++ks)
     q[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(a.q + out_row * D + 16 * ks + 8 * h));
+  // what else of the tile is looked up, its loads together: the first pages, and masks
+  const int32_t* table = a.runs.page_table + (size_t)b * a.runs.max_pages;
+  const int last_page = max(0, (s_b - 1) >> 4);
+  int base_page = blk0 * (BN / 16);
+  if constexpr (TREE) {
+    const int n_words = ((min(t.first + 32 * WR, n_tile_rows) - 1) / G - j0 + 1) * words;
+    auto mask_at = [&](int i) {
+      const int row = i / words, w = i - row * words, left = n_new - 32 * w;
+      return a.masks[(size_t)(begin + j0 + row) * a.mask_words + w] & (left >= 32 ? ~0u : (1u << left) - 1u);
+    };
+    auto page_at = [&](int i) { return base_page + i <= last_page ? table[base_page + i] : 0; };
+    const int page = RING && blk0 < blk1 ? page_at(tid) : 0;
+    const uint32_t mask = tid < n_words ? mask_at(tid) : 0u;
+    if (tid < n_words) s_masks[tid] = mask;
+    for (int i = tid + T; i < n_words; i += T) s_masks[i] = mask_at(i);
+    if (RING && blk0 < blk1) {
+      s_pages[tid] = checked_page(page, a.n_pages, a.status);
+      for (int i = tid + T; i < kRingPages; i += T)
+        if (base_page + i <= last_page) s_pages[i] = checked_page(page_at(i), a.n_pages, a.status);
+    }
+    if (kOwnKeys || RING) lds_barrier();   // (the others have one before the first block)
+  }
   // they are waited for here: a wait for their first use, inside the loop, would also wait for the
   // loads of the next block in every round
 #pragma unroll
@@ -180,8 +260,6 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   for (int i = 0; i < ND; ++i) o[i] = f32x16{};
 
   // ---- blocks: pages of the next 64 (one per lane), loads, LDS ------------------------------
-  const int32_t* table = a.runs.page_table + (size_t)b * a.runs.max_pages;
-  const int last_page = max(0, (s_b - 1) >> 4);
   int page_base = blk0 * BN / 16;
   int pages = 0;
   auto list_pages = [&](int base) {
@@ -268,15 +346,47 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
     const uint16_t* sk = s_kv + buf * 2 * kBlock + wk * BK * D;
     const uint16_t* sv = s_kv + buf * 2 * kBlock + kBlock + wk * BK * D;
     f32x16 s[KT];
+    auto key_part = [&](int kt, int ks) {
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(sk + k_at<D>(32 * kt + n, 2 * ks + h)));
+    };
+    auto value_part = [&](int step, int d) {   // of 16 keys
+      // lane i of 16 names key i / 4 of four, elements 4 * (i % 4); it gets element i of all four
+      const int row = 16 * step + 4 * h + (lane & 15) / 4;
+      const int e = 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(sv + v_at<D>(row, e)));
+      const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(sv + v_at<D>(row + 8, e)));
+      typedef short i16x8 __attribute__((ext_vector_type(8)));
+      const i16x8 va = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+      return __builtin_bit_cast(bf16x8, va);
+    };
+    // kGrouped: the reads of a row of products stand together before it (`read`: they are made by there).  Left to the
+    // compiler, whether each product waits for a read of its own depends on how many scalar registers are left.
+    constexpr bool kGrouped = TREE && WR > 1;
+    auto read = [](bf16x8& x) { asm volatile("" : "+v"(x)); };
+    bf16x8 v_part[2][ND];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       s[kt] = f32x16{};
+      if constexpr (kGrouped) {
+        bf16x8 k_part[NK];
 #pragma unroll
-      for (int ks = 0; ks < NK; ++ks) {
-        const bf16x8 ka = __builtin_bit_cast(
-            bf16x8, *reinterpret_cast<const u32x4*>(sk + k_at<D>(32 * kt + n, 2 * ks + h)));
-        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, q[ks], s[kt], 0, 0, 0);
+        for (int ks = 0; ks < NK; ++ks) k_part[ks] = key_part(kt, ks);
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) read(k_part[ks]);
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks)
+          s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_part[ks], q[ks], s[kt], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks)
+          s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_part(kt, ks), q[ks], s[kt], 0, 0, 0);
       }
+    }
+    if constexpr (kGrouped) {
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) v_part[st][d] = value_part(st, d);
     }
     {
 // a scaled score is rounded before the maximum and the difference see it: contracted into the
@@ -330,22 +440,129 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
           pw[w] = __builtin_bit_cast(uint32_t, p);
         }
         const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
+        if constexpr (kGrouped) {
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          // lane i of 16 names key i / 4 of four, elements 4 * (i % 4); it gets element i of all four
-          const int row = 32 * kt + 16 * st + 4 * h + (lane & 15) / 4;
-          const int e = 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-          const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(sv + v_at<D>(row, e)));
-          const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(sv + v_at<D>(row + 8, e)));
-          typedef short i16x8 __attribute__((ext_vector_type(8)));
-          const i16x8 va = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), pb, o[d], 0, 0, 0);
+          for (int d = 0; d < ND; ++d) read(v_part[st][d]);
+#pragma unroll
+          for (int d = 0; d < ND; ++d) {
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_part[st][d], pb, o[d], 0, 0, 0);
+            if (kt + 1 < KT) v_part[st][d] = value_part(2 * (kt + 1) + st, d);
+          }
+        } else {
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_part(2 * kt + st, d), pb, o[d], 0, 0, 0);
         }
       }
   };
 
   // ---- the walk ---------------------------------------------------------------------------
-  if (blk0 < blk1) {
+  if constexpr (RING) {
+    const uint32_t s_kv_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)s_kv;
+    constexpr int kLoads = 2 * NL;                           // of a wave and block
+    constexpr int kRaw = KV8 ? 4 * kBlock * 2 : 0;           // e4m3: where the waves' own LDS begins, in bytes
+    // a lane's 16 bytes of the rows of a load; bf16: that which stands in its place of the permuted rows (the
+    // rows of a wave's loads lie a multiple of 16 apart, or of what else the permutation knows of a row)
+    const int lr = lane / CPR, lc = lane % CPR;
+    const int row0 = wave * RPW + lr;
+    static_assert(KV8 || NW * RPW % 16 == 0, "one permutation for all loads of a wave");
+    const uint32_t k_lane = KV8 ? lane16 : (uint32_t)(lr * D * 2 + 2 * (k_at<D>(row0, lc) - row0 * D));
+    const uint32_t v_lane = KV8 ? lane16 : (uint32_t)(lr * D * 2 + 2 * (v_at<D>(row0, 8 * lc) - row0 * D));
+    auto list = [&](int first) {   // the next pages, of the blocks from `first` on
+      lds_barrier();
+      base_page = first * (BN / 16);
+      for (int i = tid; i < kRingPages; i += T)
+        if (base_page + i <= last_page) s_pages[i] = checked_page(table[base_page + i], a.n_pages, a.status);
+      lds_barrier();
+    };
+    auto issue = [&](int blk) {
+      if ((blk + 1) * (BN / 16) > base_page + kRingPages) list(blk);
+      const int stage = (blk - blk0) % kRing;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int row = row_of(i);
+        if (kPieces % T && row >= BN) break;
+        // (blocks end past the last page: it is loaded in place of those that are not)
+        // (in vector registers: scalar ones are short)
+        const uint32_t page = s_pages[min(blk * (BN / 16) + row / 16, last_page) - base_page];
+        const size_t at = ((size_t)page * (uint32_t)a.page_stride + (uint32_t)((g * 16 + row % 16) * D)) * EB;
+        const uint32_t to = s_kv_at + (KV8 ? kRaw + ((wave * kRing + stage) * NL + i) * 2048
+                                           : (stage * 2 * kBlock + row * D) * 2);
+        load_to_lds(a.k_cache + at + k_lane, to);
+        load_to_lds(a.v_cache + at + v_lane, to + (KV8 ? 1024 : kBlock * 2));
+      }
+    };
+    // waits until the loads of a block are done after which `after` more were issued
+    auto arrived = [&](int after) {
+      static_assert(kRing == 4, "cases below");
+      if (after >= 3) load_wait<3 * kLoads>();
+      else if (after == 2) load_wait<2 * kLoads>();
+      else if (after == 1) load_wait<kLoads>();
+      else load_wait<0>();
+    };
+    if (blk0 < blk1) {
+      if constexpr (KV8) {
+        const u32x4* raw = reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(s_kv) + kRaw + wave * kRing * NL * 2048 + lane16);
+        auto convert = [&](int blk) {
+          arrived(min(kRing - 1, blk1 - 1 - blk));
+          const int stage = (blk - blk0) % kRing;
+#pragma unroll
+          for (int i = 0; i < NL; ++i) {
+            kr[i] = raw[(stage * NL + i) * 128];
+            vr[i] = raw[(stage * NL + i) * 128 + 64];
+          }
+          store(blk, (blk - blk0) & 1);
+          wave_lds_sync();   // (its own LDS has been read)
+          if (blk + kRing < blk1) issue(blk + kRing);
+        };
+        for (int i = 0; i < kRing; ++i)
+          if (blk0 + i < blk1) issue(blk0 + i);
+        convert(blk0);
+        for (int blk = blk0; blk < blk1; ++blk) {
+          lds_barrier();   // the block is in LDS, and nobody reads the other buffer any more
+          if (blk + 1 < blk1) convert(blk + 1);
+          attend(blk, (blk - blk0) & 1);
+        }
+      } else {
+        for (int i = 0; i < kRing - 1; ++i)
+          if (blk0 + i < blk1) issue(blk0 + i);
+        for (int blk = blk0; blk < blk1; ++blk) {
+          const int stage = (blk - blk0) % kRing;
+          arrived(min(kRing - 2, blk1 - 1 - blk));
+          lds_barrier();   // all waves' loads of the block are done, and nobody reads the block before it any more
+          if (blk + kRing - 1 < blk1) issue(blk + kRing - 1);
+          if ((blk + 1) * BN > lim_first) {   // infinite and NaN values, see store
+            uint32_t seen = 0;
+            u32x4* sv = reinterpret_cast<u32x4*>(s_kv + stage * 2 * kBlock + kBlock);
+            u32x4 x[NL];
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+              const int at = i * T + tid;
+              if (kPieces % T && at >= kPieces) break;
+              x[i] = sv[at];
+              if (blk * BN + at / CPR >= s_b) x[i] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+              for (int w = 0; w < 4; ++w) look_for_others<KV8>(x[i][w], seen);
+            }
+            const bool some = __any(has_others<KV8>(seen));
+            others |= some;
+            if (some || (blk + 1) * BN > s_b) {
+#pragma unroll
+              for (int i = 0; i < NL; ++i) {
+                const int at = i * T + tid;
+                if (kPieces % T && at >= kPieces) break;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) x[i][w] = without_others<KV8>(x[i][w]);
+                sv[at] = x[i];
+              }
+            }
+            lds_barrier();
+          }
+          attend(blk, stage);
+        }
+      }
+    }
+  } else if (blk0 < blk1) {
     list_pages(page_base);
     load(blk0);
     store(blk0, 0);
@@ -371,13 +588,15 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
     others = *s_others != 0;
   }
   if (others) {
+    const ExtendArgs z = TREE ? read_args() : a;
+    const int32_t* table = z.runs.page_table + (size_t)b * z.runs.max_pages;
 #pragma unroll 1
     for (int blk = max(blk0, lim_first / BN); blk < blk1; ++blk)
 #pragma unroll 1
       for (int key = blk * BN + wk * BK; key < min(blk * BN + (wk + 1) * BK, lim_hi); ++key) {
-        const int page = checked_page(table[key >> 4], a.n_pages, a.status);
+        const int page = checked_page(table[key >> 4], z.n_pages, z.status);
         const bool sees = TREE ? seen_of(key) & 1u : key < lim;
-        const uint8_t* v = a.v_cache + ((size_t)page * a.page_stride + (size_t)(g * 16 + key % 16) * D) * EB;
+        const uint8_t* v = z.v_cache + ((size_t)page * z.page_stride + (size_t)(g * 16 + key % 16) * D) * EB;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -392,15 +611,18 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   }
 
   // ---- the result, or this split's part of it: outputs e .. e + 3 of the lane's row ----------
-  const float v_scale = KV8 && a.v_scale ? a.v_scale[g] : 1.f;
-  const size_t part = (size_t)split * a.runs.n_rows * Hq + out_row;
+  const ExtendArgs z = TREE ? read_args() : a;
+  const float v_scale = KV8 && z.v_scale ? z.v_scale[g] : 1.f;
+  const size_t part = piece.part + (TREE ? 32 * wr + n : out_row);
+  f32x4* part_o = reinterpret_cast<f32x4*>(z.part_o + part * D);
+  u32x2* out = reinterpret_cast<u32x2*>(z.out + out_row * D);
   auto emit = [&](const f32x4& x, int e) {
-    if (n_valid > 1) *reinterpret_cast<f32x4*>(a.part_o + part * D + e) = x;
-    else *reinterpret_cast<u32x2*>(a.out + out_row * D + e) = pack_outputs(x, v_scale, l);
+    if (!piece.whole) part_o[e / 4] = x;
+    else out[e / 4] = pack_outputs(x, v_scale, l);
   };
   auto emit_sums = [&]() {
-    if (a.n_split > 1 && split == 0) a.part_n[out_row] = n_valid > 1 ? n_valid : 0;
-    if (n_valid > 1) *reinterpret_cast<float2*>(a.part_ml + 2 * part) = make_float2(m, l);
+    if (piece.note >= 0) z.part_n[out_row] = TREE && piece.note ? piece.note | (32 * wr + n) << 20 : piece.note;
+    if (!piece.whole) *reinterpret_cast<float2*>(z.part_ml + 2 * part) = make_float2(m, l);
   };
 
   if constexpr (WK == 1) {
@@ -414,9 +636,10 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   } else {
     // Waves along the keys are joined through LDS, in their order: each takes a share of the
     // outputs (of every row) and reads it from all.
-    static_assert(WR == 1 && 4 * ND % WK == 0, "whole shares");
+    static_assert(4 * ND % WK == 0, "whole shares");
     constexpr int kShare = 4 * ND / WK;           // groups of four outputs
-    f32x4* so = reinterpret_cast<f32x4*>(s_kv);   // [WK][4 * ND][64]
+    f32x4* so = reinterpret_cast<f32x4*>(s_kv) + wr * WK * 4 * ND * 64;   // [WK][4 * ND][64] of the rows
+    s_ml += wr * WK * 64;
     lds_barrier();
     s_ml[wk * 64 + lane] = make_float2(m, l);
 #pragma unroll
@@ -446,6 +669,26 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
       emit(x, 8 * at + 4 * h);
     }
   }
+}
+
+// The piece that split blockIdx.z of KV head blockIdx.x takes of a causal tile of BM rows, in blocks of BN keys;
+// false: none.
+template <int BM, int BN>
+__device__ __forceinline__ bool causal_piece(const ExtendArgs& a, const TileOf& t, Piece& p) {
+  const int G = a.n_q_heads / a.n_kv_heads, split = blockIdx.z;
+  const int last = min(t.first + BM - 1, t.n_rows - 1) / G;
+  const int n_blocks = (max(0, t.s_b - t.n_new + last + 1) + BN - 1) / BN;
+  // pieces of one length whatever the sequence's: a short sequence has fewer
+  const int per_split = a.split_keys / BN;
+  const int n_valid = max(1, (n_blocks + per_split - 1) / per_split);
+  if (split >= n_valid) return false;
+  p.g = blockIdx.x;
+  p.blk0 = split * per_split;
+  p.blk1 = min(n_blocks, p.blk0 + per_split);
+  p.whole = n_valid == 1;
+  p.note = a.n_split > 1 && split == 0 ? (n_valid > 1 ? n_valid : 0) : -1;
+  p.part = (size_t)split * a.runs.n_rows * a.n_q_heads;
+  return true;
 }
 
 // The tile of this workgroup: which sequence, which of its rows; false: there is none.

@@ -19,8 +19,22 @@ struct TreeLayoutArgs {
 
 hipError_t launch_tree_layout(const TreeLayoutArgs& a, hipStream_t stream);
 
-ExtendPlan plan_tree(const delta_shape_t* s, int n_rows, int max_new);
-hipError_t launch_tree_attn(const ExtendPlan& p, int head_dim, bool kv8, const ExtendArgs& a, hipStream_t stream);
+// How an attention call over trees is cut: tiles of `rows` (token, query head of the group) rows per (sequence,
+// KV head).  Up to kCutBatch sequences: groups of n_kv_heads workgroups share the work evenly, from the sequences'
+// lengths; more sequences: a workgroup per tile and KV head.
+constexpr int kCutBatch = 256;
+// Work is counted in units of about 0.14 us: a tile costs kTileUnits and more for each block of its keys
+// (tree_attn_kernel.hip), and a group takes at least kLeastUnits.
+constexpr int kTileUnits = 40, kLeastUnits = 16, kMostUnits64 = 6;   // (kMostUnits64: of 64 keys)
+struct TreePlan {
+  int rows = 0;         // 32 or 256
+  int tiles = 0;        // most tiles of a call
+  int workgroups = 0;   // groups * n_kv_heads, at most 1023 groups; 0: not shared
+  bool pieces = false;  // a group takes a piece of one tile, else an equal part of all
+};
+
+TreePlan plan_tree(const delta_shape_t* s, int n_rows, int max_new);
+hipError_t launch_tree_attn(const TreePlan& p, int head_dim, bool kv8, const ExtendArgs& a, hipStream_t stream);
 
 // Pieces of a row of probabilities, each summed by a workgroup of its own.
 constexpr int kMostPieces = 64, kMostPiece = 16384;   // and their elements

@@ -10,7 +10,52 @@
 
 namespace delta {
 
-ExtendPlan plan_tree(const delta_shape_t* s, int n_rows, int max_new) { return plan_extend(s, n_rows, max_new); }
+namespace {
+
+constexpr int kCus = 256;
+
+// Most tiles of a call, whatever its longest run: every run ends in a partial tile, so at most one tile per run more
+// than whole ones.
+int64_t most_tiles(const delta_shape_t* s, int n_rows, int tile_rows) {
+  return (int64_t)n_rows * (s->n_q_heads / s->n_kv_heads) / tile_rows + std::min(s->batch, n_rows);
+}
+
+// Units of a tile of the longest sequence, most groups that fill the GPU, and most that a call with so many tiles has.
+int64_t most_units(const delta_shape_t* s) { return kTileUnits + kMostUnits64 * ((int64_t)s->max_seq_len / 64 + 4); }
+int64_t full_groups(const delta_shape_t* s) { return std::max(1, kCus / s->n_kv_heads); }
+int64_t most_groups(const delta_shape_t* s, int64_t tiles) {
+  return std::min(full_groups(s), tiles * (1 + most_units(s) / kLeastUnits) + 1);
+}
+
+}  // namespace
+
+// Tiles of 32 rows, where a group's workgroups have up to six of their blocks of 128 keys to walk: then what a tile
+// costs before and after its walk decides, and four waves start and end sooner than eight.  Measured on MI355X, us,
+// tiles of 32 and 256 rows: 28/4 heads, a tree of 16 behind 8192 tokens (4 blocks) 20.5 and 23.2, 32768 (16) 44 and
+// 34; 32/8 heads, 64 behind 2048 (4) 20.1 and 26.7; 16 sequences of 4K-16K, 16 rows each 232 and 153.
+TreePlan plan_tree(const delta_shape_t* s, int n_rows, int max_new) {
+  const int G = s->n_q_heads / s->n_kv_heads;
+  const int64_t full = full_groups(s);
+  auto tiles_of = [&](int tile_rows) {
+    const int64_t by_run = (int64_t)s->batch * (((int64_t)max_new * G + tile_rows - 1) / tile_rows);
+    return std::min(by_run, most_tiles(s, n_rows, tile_rows));
+  };
+  const bool few = (int64_t)max_new * G <= 32 ||
+                   (s->batch <= kCutBatch && tiles_of(32) * ((int64_t)s->max_seq_len / 128 + 1) <= 6 * full);
+  TreePlan p;
+  p.rows = few ? 32 : 256;
+  p.tiles = (int)tiles_of(p.rows);
+  const int64_t tiles = most_tiles(s, n_rows, p.rows);
+  // (short sequences: joining parts takes 3 us, as long as walking two or three of these blocks)
+  if (s->max_seq_len <= 768 || s->batch > kCutBatch || tiles * most_units(s) >= 1 << 30) return p;
+  // A group's units, with pieces of tiles and with equal parts of all of them, by the bound of the lengths: the
+  // first where what they are longer is less than the second tile that most equal parts touch.
+  const int64_t blocks = tiles * 4 * ((int64_t)s->max_seq_len / 64 + 4);
+  const int64_t equal = std::max<int64_t>(kLeastUnits, (blocks + kTileUnits * tiles) / full);
+  p.pieces = tiles < full && std::max<int64_t>(kLeastUnits, blocks / (full - tiles)) <= equal + kTileUnits;
+  p.workgroups = s->n_kv_heads * (int)most_groups(s, tiles);
+  return p;
+}
 
 }  // namespace delta
 
@@ -26,7 +71,24 @@ int check_drafts(int32_t batch, int32_t n_rows, int32_t max_new, const int32_t* 
   return DELTA_OK;
 }
 
-int tree_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, ExtendLayout* L) {
+struct TreeLayout {
+  TreePlan plan;
+  int n_rows = 0;   // rows that can belong to a run
+  size_t status = 0, part_ml = 0, part_n = 0, part_o = 0, total = 0;
+};
+
+// Bytes of a call's workspace; every workgroup of a shared call has room for two parts of a tile.
+size_t lay_out(const delta_shape_t* s, int n_rows, const TreePlan& p, TreeLayout* L) {
+  const size_t parts = 2 * (size_t)p.workgroups * p.rows, rows = p.workgroups ? (size_t)n_rows * s->n_q_heads : 0;
+  size_t off = 0;
+  L->status = off;  off = align_up(off + sizeof(uint32_t));
+  L->part_ml = off; off = align_up(off + sizeof(float) * 2 * parts);
+  L->part_n = off;  off = align_up(off + sizeof(int32_t) * rows);
+  L->part_o = off;  off = align_up(off + sizeof(float) * s->head_dim * parts);
+  return off;
+}
+
+int tree_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, TreeLayout* L) {
   int rc = check_shape(s);
   if (rc) return rc;
   if (n_rows < 0 || max_new < 0 || max_new > n_rows) return DELTA_ERR_INVALID_ARG;
@@ -35,9 +97,7 @@ int tree_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, ExtendL
   L->n_rows = (int)std::min<int64_t>(n_rows, (int64_t)s->batch * max_new);
   L->plan = plan_tree(s, L->n_rows, max_new);
   if (L->plan.tiles > kMostTiles) return DELTA_ERR_UNSUPPORTED;
-  const size_t rows = (size_t)L->n_rows * s->n_q_heads;
-  if (L->plan.n_split > 1) L->total = lay_out(rows, L->plan.n_split * rows, s->head_dim, L);
-  else L->total = lay_out(0, 0, s->head_dim, L);
+  L->total = lay_out(s, L->n_rows, L->plan, L);
   return DELTA_OK;
 }
 
@@ -82,18 +142,23 @@ int delta_tree_layout(const delta_shape_t* shape, const int32_t* seq_lens, int32
 
 int delta_tree_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int32_t max_new, size_t* out) {
   if (!out) return DELTA_ERR_INVALID_ARG;
-  ExtendLayout L;
+  TreeLayout L;
   int rc = tree_layout(shape, n_rows, max_new, &L);
   if (rc) return rc;
-  const size_t rows = (size_t)L.n_rows * shape->n_q_heads, most = kMostParts;
-  *out = lay_out(std::min(rows, most), std::min(kMostSplits * rows, most), shape->head_dim, &L);
+  // of either tile: a smaller call may take the smaller one, of which there are more
+  *out = L.total;
+  TreePlan p = L.plan;
+  for (p.rows = 32; p.rows <= L.plan.rows; p.rows *= 8) {
+    p.workgroups = shape->n_kv_heads * (int)most_groups(shape, most_tiles(shape, L.n_rows, p.rows));
+    *out = std::max(*out, lay_out(shape, L.n_rows, p, &L));
+  }
   return DELTA_OK;
 }
 
 int delta_tree_attn(const delta_shape_t* shape, const delta_kv_t* kv, int32_t n_rows, int32_t max_new,
                     const int32_t* row_offsets, const uint32_t* masks, int32_t mask_words, const void* q,
                     void* out, void* ws, size_t ws_bytes, void* stream) {
-  ExtendLayout L;
+  TreeLayout L;
   int rc = tree_layout(shape, n_rows, max_new, &L);
   if (rc) return rc;
   if ((rc = check_kv(kv))) return rc;
@@ -107,7 +172,12 @@ int delta_tree_attn(const delta_shape_t* shape, const delta_kv_t* kv, int32_t n_
   for (const void* p : {q, static_cast<const void*>(out), kv->k_cache, kv->v_cache})
     if (!aligned(p, 16)) return DELTA_ERR_INVALID_ARG;
   if (!aligned(ws, 256)) return DELTA_ERR_INVALID_ARG;
-  ExtendArgs a = extend_args(shape, kv, L, row_offsets, q, out, ws);
+  char* w = static_cast<char*>(ws);
+  ExtendArgs a = extend_args(shape, kv, L.n_rows, row_offsets, q, out);
+  a.part_ml = reinterpret_cast<float*>(w + L.part_ml);
+  a.part_o = reinterpret_cast<float*>(w + L.part_o);
+  a.part_n = reinterpret_cast<int32_t*>(w + L.part_n);
+  a.status = reinterpret_cast<uint32_t*>(w + L.status);
   a.masks = masks;
   a.mask_words = mask_words;
   return hip_rc(launch_tree_attn(L.plan, shape->head_dim, is_e4m3(kv), a, static_cast<hipStream_t>(stream)));

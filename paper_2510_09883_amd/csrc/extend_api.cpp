@@ -10,6 +10,10 @@
 
 namespace delta {
 
+// Most pieces that a call's keys are cut into, and most (row, query head) parts of outputs that it
+// keeps (68 MB at head size 128): with the second a call's workspace grows with its rows and nothing
+// else, so that one sized for the most rows serves every smaller call.
+constexpr int kMostSplits = 32, kMostParts = 1 << 17;
 // Which kernel, and into how many pieces the keys are cut.  The host knows no run but the longest, so
 // it takes the rows for runs of that length and single tokens.
 //
@@ -64,6 +68,22 @@ ExtendPlan plan_extend(const delta_shape_t* s, int n_rows, int max_new) {
 namespace {
 
 using namespace delta;
+
+struct ExtendLayout {
+  ExtendPlan plan;
+  int n_rows = 0;   // rows that can belong to a run
+  size_t status = 0, part_ml = 0, part_n = 0, part_o = 0, total = 0;
+};
+
+// Bytes of `rows` (row, query head) pairs in `parts` parts.
+size_t lay_out(size_t rows, size_t parts, int head_dim, ExtendLayout* L) {
+  size_t off = 0;
+  L->status = off;  off = align_up(off + sizeof(uint32_t));
+  L->part_ml = off; off = align_up(off + sizeof(float) * 2 * parts);
+  L->part_n = off;  off = align_up(off + sizeof(int32_t) * rows);
+  L->part_o = off;  off = align_up(off + sizeof(float) * head_dim * parts);
+  return off;
+}
 
 int extend_layout(const delta_shape_t* s, int32_t n_rows, int32_t max_new, ExtendLayout* L) {
   int rc = check_shape(s);
@@ -121,7 +141,14 @@ int delta_extend_attn(const delta_shape_t* shape, const delta_kv_t* kv, int32_t 
   for (const void* p : {q, static_cast<const void*>(out), kv->k_cache, kv->v_cache})
     if (!aligned(p, 16)) return DELTA_ERR_INVALID_ARG;
   if (!aligned(ws, 256)) return DELTA_ERR_INVALID_ARG;
-  const ExtendArgs a = extend_args(shape, kv, L, row_offsets, q, out, ws);
+  char* w = static_cast<char*>(ws);
+  ExtendArgs a = extend_args(shape, kv, L.n_rows, row_offsets, q, out);
+  a.part_ml = reinterpret_cast<float*>(w + L.part_ml);
+  a.part_o = reinterpret_cast<float*>(w + L.part_o);
+  a.part_n = reinterpret_cast<int32_t*>(w + L.part_n);
+  a.n_split = L.plan.n_split;
+  a.split_keys = L.plan.split_keys;
+  a.status = reinterpret_cast<uint32_t*>(w + L.status);
   return hip_rc(launch_extend(L.plan, shape->head_dim, is_e4m3(kv), a, static_cast<hipStream_t>(stream)));
 }
 

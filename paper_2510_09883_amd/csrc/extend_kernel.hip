@@ -44,7 +44,9 @@ __global__ __launch_bounds__(256, 2) void extend_few_kernel(const ExtendArgs a) 
   __shared__ __attribute__((aligned(256))) uint16_t s_kv[kBodyLds<D, 1, 4, 1> / 2];
   __shared__ float2 s_ml[4 * 64];
   TileOf t;
-  if (find_tile<32>(a, t)) extend_body<D, 1, 4, 1, KV8, false>(a, t, s_kv, s_ml, nullptr);
+  Piece p;
+  if (find_tile<32>(a, t) && causal_piece<32, 128>(a, t, p))
+    extend_body<D, 1, 4, 1, KV8, false>(a, t, p, s_kv, s_ml, nullptr);
 }
 
 // Tiles of 256 rows, eight waves along them; a tile that has no more than 32 (a single token beside
@@ -57,8 +59,12 @@ __global__ __launch_bounds__(512, 1) void extend_many_kernel(const ExtendArgs a)
   TileOf t;
   if (!find_tile<256>(a, t)) return;
   if (threadIdx.x == 0) s_others = 0;   // (the walk's first barrier is before any use)
-  if (t.n_rows - t.first <= 32) extend_body<D, 1, 8, 1, KV8, false>(a, t, s_kv, s_ml, nullptr);
-  else extend_body<D, 8, 1, 2, KV8, false>(a, t, s_kv, s_ml, &s_others);
+  Piece p;
+  if (t.n_rows - t.first <= 32) {
+    if (causal_piece<32, 256>(a, t, p)) extend_body<D, 1, 8, 1, KV8, false>(a, t, p, s_kv, s_ml, nullptr);
+  } else {
+    if (causal_piece<256, 64>(a, t, p)) extend_body<D, 8, 1, 2, KV8, false>(a, t, p, s_kv, s_ml, &s_others);
+  }
 }
 
 template <int D, bool KV8>

@@ -21,56 +21,30 @@ inline Runs runs_of(const delta_shape_t* s, const delta_kv_t* kv, int32_t n_rows
   return Runs{row_offsets, kv->seq_lens, kv->page_table, n_rows, s->batch, s->max_pages_per_seq};
 }
 
-// Most pieces that a call's keys are cut into, and most (row, query head) parts of outputs that it
-// keeps (68 MB at head size 128): with the second a call's workspace grows with its rows and nothing
-// else, so that one sized for the most rows serves every smaller call.
-constexpr int kMostSplits = 32, kMostParts = 1 << 17;
 // Most tiles of a call: a launch's second grid size.
 constexpr int kMostTiles = 65535;
 // The longest bound of a sequence: the kernels round key indices up to whole blocks, of 256 keys at
 // most, in 32 bits.
 constexpr int kMostKeys = INT32_MAX - 511;
 
-struct ExtendLayout {
-  ExtendPlan plan;
-  int n_rows = 0;   // rows that can belong to a run
-  size_t status = 0, part_ml = 0, part_n = 0, part_o = 0, total = 0;
-};
-
-// Bytes of `rows` (row, query head) pairs in `parts` parts.
-inline size_t lay_out(size_t rows, size_t parts, int head_dim, ExtendLayout* L) {
-  size_t off = 0;
-  L->status = off;  off = align_up(off + sizeof(uint32_t));
-  L->part_ml = off; off = align_up(off + sizeof(float) * 2 * parts);
-  L->part_n = off;  off = align_up(off + sizeof(int32_t) * rows);
-  L->part_o = off;  off = align_up(off + sizeof(float) * head_dim * parts);
-  return off;
-}
-
-// The kernels' arguments of an attention call whose own have been checked.
-inline ExtendArgs extend_args(const delta_shape_t* shape, const delta_kv_t* kv, const ExtendLayout& L,
-                              const int32_t* row_offsets, const void* q, void* out, void* ws) {
-  char* w = static_cast<char*>(ws);
+// The kernels' arguments of an attention call whose own have been checked, but for the cut and the workspace.
+inline ExtendArgs extend_args(const delta_shape_t* shape, const delta_kv_t* kv, int n_rows, const int32_t* row_offsets,
+                              const void* q, void* out) {
   ExtendArgs a{};
-  a.runs = runs_of(shape, kv, L.n_rows, row_offsets);
+  a.runs = runs_of(shape, kv, n_rows, row_offsets);
   a.k_cache = static_cast<const uint8_t*>(kv->k_cache);
   a.v_cache = static_cast<const uint8_t*>(kv->v_cache);
   a.k_scale = kv->k_scale;
   a.v_scale = kv->v_scale;
   a.q = static_cast<const uint16_t*>(q);
   a.out = static_cast<uint16_t*>(out);
-  a.part_ml = reinterpret_cast<float*>(w + L.part_ml);
-  a.part_o = reinterpret_cast<float*>(w + L.part_o);
-  a.part_n = reinterpret_cast<int32_t*>(w + L.part_n);
   a.page_stride = (int64_t)shape->n_kv_heads * 16 * shape->head_dim;
   a.n_q_heads = shape->n_q_heads;
   a.n_kv_heads = shape->n_kv_heads;
   a.max_seq_len = shape->max_seq_len;
-  a.n_split = L.plan.n_split;
-  a.split_keys = L.plan.split_keys;
+  a.n_split = 1;
   a.scale_log2 = scale_log2(shape);
   a.n_pages = kv->n_pages;
-  a.status = reinterpret_cast<uint32_t*>(w + L.status);
   return a;
 }
 
