@@ -107,9 +107,9 @@ int delta_verify_workspace_bytes(int32_t batch, int32_t vocab, size_t* out);
  *   n_path:  int32 [batch]: their count (0: the run is empty, next is -1)
  *   next:    int32 [batch]
  *   max_new: at least the longest run, at least 1 and at most n_rows (of longer runs the rest is not tried)
- *   ws:      256-byte aligned, zero-filled once after allocation; every call leaves it ready for the next.
- *            Calls that share one must not run concurrently.
- * batch at most 65535, vocab at most 2^20 and n_rows below 2^24, else DELTA_ERR_UNSUPPORTED. */
+ *   ws:      256-byte aligned, of any content; it keeps nothing between calls.  Calls that share one must not
+ *            run concurrently.
+ * Two kernel launches.  batch at most 65535, vocab at most 2^20 and n_rows below 2^24, else DELTA_ERR_UNSUPPORTED. */
 int delta_verify_drafts(int32_t batch, int32_t n_rows, int32_t max_new, const int32_t* row_offsets, int32_t vocab,
                         const float* target, int64_t target_row_stride, const float* draft,
                         int64_t draft_row_stride, const int32_t* tokens, const int32_t* parents,

@@ -36,16 +36,16 @@ struct TreePlan {
 TreePlan plan_tree(const delta_shape_t* s, int n_rows, int max_new);
 hipError_t launch_tree_attn(const TreePlan& p, int head_dim, bool kv8, const ExtendArgs& a, hipStream_t stream);
 
-// Pieces of a row of probabilities, each summed by a workgroup of its own.
-constexpr int kMostPieces = 64, kMostPiece = 16384;   // and their elements
+// Pieces of a row of probabilities, each taken by a workgroup of eight waves, and the elements of a piece and of a
+// wave's part of it.
+constexpr int kMostPieces = 64, kVerifyWaves = 8, kMostPart = 2048, kMostPiece = kVerifyWaves * kMostPart;
 constexpr int kMostVocab = kMostPieces * kMostPiece;
 
-// A sequence's part of the workspace: at a place that does not depend on the batch, so that calls of any size
-// leave the counters of all zero.
+// A sequence's part of the workspace, from the first launch to the second.
 struct VerifyState {
-  int32_t arrived;           // workgroups that are done; zero between launches
-  int32_t pad[kCounterStride - 1];
-  double sums[kMostPieces][2];   // a piece's sums of r and of p
+  int32_t cur, k;                            // the last accepted row and the rejections at it
+  double left[kMostDrafts];                  // R before each of them, of drawn drafts
+  double sums[kMostPieces * kVerifyWaves];   // a part's sum of r
 };
 
 struct VerifyArgs {
@@ -61,6 +61,7 @@ struct VerifyArgs {
   int32_t* next;             // [batch]
   VerifyState* state;        // [batch]
   int32_t vocab, max_new;
+  int32_t part;              // elements of a wave's part: a multiple of for_row's round
   int32_t n_pieces;          // workgroups per sequence
 };
 

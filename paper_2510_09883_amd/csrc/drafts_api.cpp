@@ -218,7 +218,13 @@ int delta_verify_drafts(int32_t batch, int32_t n_rows, int32_t max_new, const in
   a.state = static_cast<VerifyState*>(ws);
   a.vocab = vocab;
   a.max_new = max_new;
-  a.n_pieces = std::max(ceil_div(vocab, kMostPiece), std::min({ceil_div(1024, batch), ceil_div(vocab, 2048), kMostPieces}));
+  // one round of loads a wave; two where that would be more workgroups than fit the GPU at once
+  a.part = kMostPart / 2;
+  a.n_pieces = ceil_div(vocab, kVerifyWaves * a.part);
+  if (a.n_pieces > kMostPieces || (int64_t)a.n_pieces * batch > 1536) {
+    a.part = kMostPart;
+    a.n_pieces = ceil_div(vocab, kVerifyWaves * a.part);
+  }
   return hip_rc(launch_verify(a, static_cast<hipStream_t>(stream)));
 }
 

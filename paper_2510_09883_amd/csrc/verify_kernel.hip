@@ -11,11 +11,12 @@
 // tests need of the probabilities is one value of the target and one of the drafting model per row, all loaded
 // at once, and the rest is comparisons in LDS; rows are tried in ascending order, the current row's next child
 // found by a ballot.  (Only where drawn siblings are tried after a rejection does R have to be summed over a
-// whole row on the way, by each workgroup for itself.)  Then each sums its piece of the last current row's
-// residual, and the one that is done last finds the piece, and in it the token, at which the partial sums pass
-// u0 R.  Every sum has a fixed order, so equal calls give equal tokens whichever workgroup is last.
+// whole row on the way, by each workgroup for itself.)  Then each wave sums its part of the last current row's
+// residual.  A second launch finds the part, and in it the token, at which the partial sums pass u0 R.  Every sum
+// has a fixed order, so equal calls give equal tokens.
 //
-// Bound: launch and the chain offsets -> parents -> values for few sequences, HBM for many.
+// Bound: latencies, of launches and of the chains offsets -> parents -> values -> row and sums -> row; then the
+// reads of the rows.
 #include <algorithm>
 
 #include "drafts.h"
@@ -24,25 +25,51 @@
 namespace delta {
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;
-constexpr int kWindow = 4 * kThreads;            // elements searched at once
+constexpr int kWaves = kVerifyWaves, kThreads = 64 * kWaves;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+// x of another lane of the row, or of another row (0 where there is none): see wave_incl_scan.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Inclusive prefix sums over the 64 lanes.
+__device__ __forceinline__ double wave_scan(double x) {
+  x += moved<0x111, 0xf>(x);
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  x += moved<0x142, 0xa>(x);
+  x += moved<0x143, 0xc>(x);
   return x;
 }
+__device__ __forceinline__ double lane_of(double x, int lane) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)w, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(w >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double x) { return lane_of(wave_scan(x), 63); }
 
 struct Shared {
   int16_t parent[kMostDrafts];     // -1: never tried
   int32_t token[kMostDrafts];
   float uniform[kMostDrafts], p[kMostDrafts], q[kMostDrafts];
   double left[kMostDrafts];        // R before each rejection at the current row
-  double wave[2 * kWaves];
+  double wave[kWaves];
   uint32_t dropped[kMostPiece / 32];   // tokens of the piece that were rejected (draft == null)
-  double window[kWindow];
-  double sums[2 * kMostPieces];
-  int found, last;
+};
+
+struct SharedPick {
+  double left[kMostDrafts];
+  double wave[kWaves], before;
+  double part[kMostPieces * kWaves];   // sums of p, where they are needed
+  uint32_t dropped[kMostPiece / 32];
+  double window[kMostPart];
+  int past[kWaves], some[kWaves];
 };
 
 // The sum over all threads of x, in all of them, in a fixed order.
@@ -57,12 +84,121 @@ __device__ __forceinline__ double block_sum(double x, double* s_wave) {
   return sum;
 }
 
-// r after k rejections of drawn drafts (NaN and negative values count as 0).
+// Inclusive prefix sums over the threads, what stands before the thread, and the sum, each in a fixed order.
+__device__ __forceinline__ double block_scan(double x, double* s_wave, double* incl, double* excl) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const double sum = wave_scan(x);
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = sum;
+  __syncthreads();
+  double waves = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) waves += s_wave[w];
+    all += s_wave[w];
+  }
+  *incl = waves + sum;
+  const double before = __shfl_up(sum, 1);
+  *excl = waves + (lane ? before : 0.0);
+  return all;
+}
+
+// f(v, p[v], q[v]) for the elements first .. end - 1, which THREADS threads share, t the caller's number among them.
+// In full rounds a thread has 16 elements of each row under way; 16 bytes at once where the rows are aligned to them
+// (first is a multiple of 4).
+template <int THREADS, class F>
+__device__ __forceinline__ void for_row(const float* p, const float* q, int first, int end, int t, F f) {
+  constexpr int kRound = 16 * THREADS;
+  int v = first;
+  if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15) == 0) {
+    for (; v + kRound <= end; v += kRound) {
+      f32x4 x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = v + 4 * (i * THREADS + t);
+        x[i] = *reinterpret_cast<const f32x4*>(p + at);
+        if (q) y[i] = *reinterpret_cast<const f32x4*>(q + at);
+        else y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) f(v + 4 * (i * THREADS + t) + c, x[i][c], y[i][c]);
+    }
+  } else {
+    for (; v + kRound <= end; v += kRound) {
+      float x[16], y[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[i] = p[v + i * THREADS + t];
+        y[i] = q ? q[v + i * THREADS + t] : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f(v + i * THREADS + t, x[i], y[i]);
+    }
+  }
+  if (v >= end) return;
+  float x[16], y[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {   // (past the end: the last element again, not counted)
+    const int at = min(v + i * THREADS + t, end - 1);
+    x[i] = p[at];
+    y[i] = q ? q[at] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (v + i * THREADS + t < end) f(v + i * THREADS + t, x[i], y[i]);
+}
+
+// A probability; negative and NaN ones count as 0.
+__device__ __forceinline__ double mass_of(float x) { return fmaxf(x, 0.f); }
+
+// r after k rejections of drawn drafts.
 __device__ __forceinline__ double residual(float p, float q, int k, const double* left) {
-  double r = fmax((double)p, 0.0);
-  for (int i = 0; i < k; ++i) r = fmax(r - left[i] * (double)q, 0.0);
+  double r = mass_of(p);
+  if (k) r = fmax(r - mass_of(q), 0.0);   // (left[0] is 1)
+  for (int i = 1; i < k; ++i) r = fmax(r - left[i] * mass_of(q), 0.0);
   return r;
 }
+
+// The current row's probabilities after k rejections, in pieces and waves' parts of them.
+struct Row {
+  const float *p, *q;          // q: null where it is not needed
+  int vocab, part, per;        // elements of a part and of a piece
+  int k;
+  bool drawn;
+  const double* left;          // LDS
+  uint32_t* dropped;           // LDS: rejected tokens of a piece, if they were not drawn
+
+  __device__ __forceinline__ Row(const VerifyArgs& a, int begin, int cur, int k, const double* left, uint32_t* dropped)
+      : p(a.target + (int64_t)(begin + cur) * a.target_stride),
+        q(a.draft && k ? a.draft + (int64_t)(begin + cur) * a.draft_stride : nullptr),
+        vocab(a.vocab), k(k), drawn(a.draft != nullptr), left(left), dropped(dropped) {
+    part = a.part;
+    per = part * kWaves;
+  }
+  __device__ __forceinline__ int begin_of(int i) const { return min(i * part, vocab); }
+  __device__ __forceinline__ int end_of(int i) const { return min((i + 1) * part, vocab); }
+  // Notes the rejected tokens from v0 on: tokens of rows cur + 1 .. n - 1 whose parent is cur.
+  template <class Parent, class Token>
+  __device__ __forceinline__ void mark_dropped(int v0, int cur, int n, Parent parent, Token token) const {
+    if (drawn || !k) return;
+    const int v1 = min(v0 + per, vocab);
+    for (int i = threadIdx.x; i < (per + 31) / 32; i += kThreads) dropped[i] = 0;
+    __syncthreads();
+    for (int j = cur + 1 + threadIdx.x; j < n; j += kThreads)
+      if (parent(j) == cur) {
+        const int x = token(j);
+        if (x >= v0 && x < v1) atomicOr(&dropped[(x - v0) >> 5], 1u << ((x - v0) & 31));
+      }
+    __syncthreads();
+  }
+  // r of element v of the piece from v0 on
+  __device__ __forceinline__ double r_of(int v, float x, float y, int v0) const {
+    if (drawn) return residual(x, y, k, left);
+    return k && (dropped[(v - v0) >> 5] >> ((v - v0) & 31) & 1) ? 0.0 : mass_of(x);
+  }
+};
 
 __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
   __shared__ Shared s;
@@ -88,7 +224,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
     s.token[j] = x;
     s.uniform[j] = a.uniform[begin + j];
     s.p[j] = some ? target[(int64_t)parent * a.target_stride + x] : 0.f;
-    s.q[j] = draft ? some ? draft[(int64_t)parent * a.draft_stride + x] : 0.f : 1.f;
+    s.q[j] = draft ? some ? fmaxf(draft[(int64_t)parent * a.draft_stride + x], 0.f) : 0.f : 1.f;
   }
   __syncthreads();
 
@@ -104,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
     const float* p = target + (int64_t)cur * a.target_stride;
     const float* q = draft + (int64_t)cur * a.draft_stride;
     double sum = 0;
-    for (int v = tid; v < a.vocab; v += kThreads) sum += residual(p[v], q[v], summed + 1, s.left);
+    for_row<kThreads>(p, q, 0, a.vocab, tid, [&](int, float x, float y) { sum += residual(x, y, summed + 1, s.left); });
     sum = block_sum(sum, s.wave);
     ++summed;
     if (tid == 0) s.left[summed] = sum;
@@ -122,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
         r = residual(s.p[j], s.q[j], k, s.left);
         mass = s.left[k];
       } else {
-        r = fmax((double)s.p[j], 0.0);
+        r = mass_of(s.p[j]);
         mass = left;
         bool again = false;   // a sibling with this token has been rejected
         if (k)
@@ -151,140 +287,121 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
     if (tid == 0) a.n_path[b] = count;
   }
 
-  // ---- sums of r and of p over this workgroup's piece
-  const float* p = target + (int64_t)cur * a.target_stride;
-  const float* q = draft && k ? draft + (int64_t)cur * a.draft_stride : nullptr;
-  const int per = (a.vocab + a.n_pieces - 1) / a.n_pieces;
-  auto mark_dropped = [&](int v0, int v1) {   // rejected tokens of [v0, v1)
-    if (draft || !k) return;
-    for (int i = tid; i < (v1 - v0 + 31) / 32; i += kThreads) s.dropped[i] = 0;
-    __syncthreads();
-    for (int j = cur + 1 + tid; j < n; j += kThreads) {
-      const int x = s.token[j];
-      if (s.parent[j] == cur && x >= v0 && x < v1) atomicOr(&s.dropped[(x - v0) >> 5], 1u << ((x - v0) & 31));
-    }
-    __syncthreads();
-  };
-  auto r_of = [&](int v, int v0) {
-    if (draft) return residual(p[v], q ? q[v] : 0.f, k, s.left);
-    const double r = fmax((double)p[v], 0.0);
-    return k && (s.dropped[(v - v0) >> 5] >> ((v - v0) & 31) & 1) ? 0.0 : r;
-  };
-  {
-    const int v0 = min(piece * per, a.vocab), v1 = min(v0 + per, a.vocab);
-    mark_dropped(v0, v1);
-    double sum_r = 0, sum_p = 0;
-    for (int v = v0 + tid; v < v1; v += kThreads) {
-      sum_r += r_of(v, v0);
-      sum_p += fmax((double)p[v], 0.0);
-    }
-    sum_r = block_sum(sum_r, s.wave);
-    sum_p = block_sum(sum_p, s.wave);
-    if (tid == 0) {
-      double* out = a.state[b].sums[piece];
-      __hip_atomic_store(out, sum_r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(out + 1, sum_p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      int32_t* counter = &a.state[b].arrived;
-      const int arrived = __hip_atomic_fetch_add(counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-      s.last = arrived == a.n_pieces - 1;
-      if (s.last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next call
-    }
-    __syncthreads();
-    if (!s.last) return;
+  // ---- the sum of r over this workgroup's piece, a part of it by each wave
+  const Row row(a, begin, cur, k, s.left, s.dropped);
+  const int v0 = piece * row.per, mine = piece * kWaves + (tid >> 6);
+  row.mark_dropped(v0, cur, n, [&](int j) { return (int)s.parent[j]; }, [&](int j) { return s.token[j]; });
+  double sum = 0;
+  for_row<64>(row.p, row.q, row.begin_of(mine), row.end_of(mine), lane, [&](int v, float x, float y) { sum += row.r_of(v, x, y, v0); });
+  sum = wave_sum(sum);
+  VerifyState& state = a.state[b];
+  if (lane == 0) state.sums[mine] = sum;
+  if (piece == 0) {
+    if (tid == 0) state.cur = cur, state.k = k;
+    if (draft)
+      for (int i = tid; i < k; i += kThreads) state.left[i] = s.left[i];
   }
+}
 
-  // ---- the last one: the piece in which the partial sums pass u0 times the whole
-  if (tid < 2 * a.n_pieces)
-    s.sums[tid] = __hip_atomic_load(&a.state[b].sums[0][0] + tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  double total = 0, total_p = 0;
-  for (int i = 0; i < a.n_pieces; ++i) total += s.sums[2 * i], total_p += s.sums[2 * i + 1];
+// The token after the accepted rows: the part, and in it the element, at which the partial sums of r pass u0 times
+// the whole.  A workgroup takes a sequence.
+__global__ __launch_bounds__(kThreads) void verify_pick_kernel(const VerifyArgs a) {
+  __shared__ SharedPick s;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int n_parts = a.n_pieces * kWaves;
+  const VerifyState& state = a.state[b];
+  // (loaded together; of an empty run they are anything)
+  const int begin = run_offset(a.runs, b), n = min(run_offset(a.runs, b + 1) - begin, a.max_new);
+  const int cur = state.cur, k = state.k;
+  double part_sum = tid < n_parts ? state.sums[tid] : 0.0;
+  if (n <= 0) return;
+  const double u0 = a.uniform[begin];
+  if (a.draft)
+    for (int i = tid; i < k; i += kThreads) s.left[i] = state.left[i];   // (the scan has barriers)
+  const Row row(a, begin, cur, k, s.left, s.dropped);
+  double incl, excl;
+  double total = block_scan(part_sum, s.wave, &incl, &excl);
   const bool use_p = !(total > 0);
-  if (use_p) total = total_p;
-  if (!(total > 0)) {
-    if (tid == 0) a.next[b] = -1;
-    return;
-  }
-  const double goal = (double)s.uniform[0] * total;
-  double before = 0, cum = 0;
-  int where = 0;
-  for (int i = 0; i < a.n_pieces; ++i) {
-    const double x = s.sums[2 * i + use_p];
-    if (x > 0) {
-      where = i;
-      before = cum;
-      if (cum + x > goal) break;
-    }
-    cum += x;
-  }
-  const int v0 = min(where * per, a.vocab), v1 = min(v0 + per, a.vocab);
-  mark_dropped(v0, v1);
-
-  // ---- the token: windows of the piece, four elements in a row per thread
-  int last_some = v0;   // the last token with r > 0 so far
-  for (int w0 = v0; w0 < v1; w0 += kWindow) {
-    __syncthreads();
-    if (tid == 0) s.found = INT32_MAX, s.last = -1;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int v = w0 + i * kThreads + tid;
-      s.window[i * kThreads + tid] = v >= v1 ? 0.0 : use_p ? fmax((double)p[v], 0.0) : r_of(v, v0);
+  if (use_p) {   // (nothing is left: p takes the place of r)
+    for (int i = tid >> 6; i < n_parts; i += kWaves) {
+      double sum = 0;
+      for_row<64>(row.p, nullptr, row.begin_of(i), row.end_of(i), lane, [&](int, float x, float) { sum += mass_of(x); });
+      sum = wave_sum(sum);
+      if (lane == 0) s.part[i] = sum;
     }
     __syncthreads();
-    double x[4], own = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = s.window[4 * tid + i];
-      own += x[i];
-    }
-    double incl = own;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const double y = __shfl_up(incl, d);
-      if (lane >= d) incl += y;
-    }
-    if (lane == 63) s.wave[tid >> 6] = incl;
-    __syncthreads();
-    double waves = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < tid >> 6) waves += s.wave[w];
-      all += s.wave[w];
-    }
-    double excl = __shfl_up(incl, 1);
-    if (lane == 0) excl = 0;
-    if (own > 0 && before + (waves + incl) > goal) {
-      double c = before + (waves + excl);
-      int v = -1;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (x[i] > 0 && (v < 0 || !(c > goal))) v = w0 + 4 * tid + i;   // (the first that passes, else the last > 0)
-        c += x[i];
-      }
-      atomicMin(&s.found, v);
-    }
-    if (own > 0) {
-      int v = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (x[i] > 0) v = w0 + 4 * tid + i;
-      atomicMax(&s.last, v);
-    }
-    __syncthreads();
-    if (s.found != INT32_MAX) {
-      if (tid == 0) a.next[b] = s.found;
+    part_sum = tid < n_parts ? s.part[tid] : 0.0;
+    total = block_scan(part_sum, s.wave, &incl, &excl);
+    if (!(total > 0)) {
+      if (tid == 0) a.next[b] = -1;
       return;
     }
-    if (s.last >= 0) last_some = s.last;
-    before += all;
   }
-  if (tid == 0) a.next[b] = last_some;
+  const double goal = u0 * total;
+  // the thread whose own numbers pass the goal first, or else the last that has any
+  auto first_past = [&](double before, double own) {
+    const uint64_t some = __ballot(own > 0), past = __ballot(own > 0 && before + incl > goal);
+    if (lane == 0) {
+      s.past[tid >> 6] = past ? tid + __builtin_ctzll(past) : INT32_MAX;
+      s.some[tid >> 6] = some ? tid + 63 - __builtin_clzll(some) : -1;
+    }
+    __syncthreads();
+    int found = INT32_MAX, last = -1;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      found = min(found, s.past[w]);
+      last = max(last, s.some[w]);
+    }
+    return found != INT32_MAX ? found : last;
+  };
+  const int where = first_past(0, part_sum);
+  if (tid == where) s.before = excl;
+
+  // ---- the token: the part's elements, four in a row per thread
+  const int v0 = row.begin_of(where), v1 = row.end_of(where), piece0 = where / kWaves * row.per;
+  static_assert(kMostPart == 4 * kThreads, "four elements a thread");
+  float x[4], y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int v = min(v0 + i * kThreads + tid, v1 - 1);
+    x[i] = row.p[v];
+    y[i] = row.q && !use_p ? row.q[v] : 0.f;
+  }
+  row.mark_dropped(piece0, cur, n, [&](int j) { return a.parents[begin + j]; }, [&](int j) { return a.tokens[begin + j]; });
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int v = v0 + i * kThreads + tid;
+    s.window[i * kThreads + tid] = v >= v1 ? 0.0 : use_p ? mass_of(x[i]) : row.r_of(v, x[i], y[i], piece0);
+  }
+  __syncthreads();
+  const double before = s.before;
+  double r[4], own = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = s.window[4 * tid + i];
+    own += r[i];
+  }
+  block_scan(own, s.wave, &incl, &excl);
+  if (tid == first_past(before, own)) {
+    double c = before + excl;
+    int v = 0;
+    bool some = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {   // the first that passes, else the last > 0
+      if (r[i] > 0 && (!some || !(c > goal))) v = 4 * tid + i, some = true;
+      c += r[i];
+    }
+    a.next[b] = v0 + v;
+  }
 }
 
 }  // namespace
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(verify_kernel, dim3(a.n_pieces, a.runs.batch), dim3(kThreads), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(verify_pick_kernel, dim3(a.runs.batch), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

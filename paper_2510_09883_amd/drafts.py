@@ -150,7 +150,7 @@ def delta_verify_workspace_bytes(batch: int, vocab: int) -> int:
 
 
 def alloc_verify_workspace(batch, vocab, device="cuda") -> torch.Tensor:
-    """A zero-filled workspace (uint8) large enough for delta_verify_drafts calls of up to so many sequences
+    """A workspace (uint8) large enough for delta_verify_drafts calls of up to so many sequences
     and tokens of the vocabulary."""
     return torch.zeros(delta_verify_workspace_bytes(batch, vocab), dtype=torch.uint8, device=device)
 
