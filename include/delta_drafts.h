@@ -94,6 +94,8 @@ int delta_verify_workspace_bytes(int32_t batch, int32_t vocab, size_t* out);
  *     next = the smallest v with r(0) + .. + r(v) > u0 * (r(0) + .. + r(vocab - 1)),
  * u0 the uniform number of the run's first row (the last token with r > 0 if there is no such v).  Where r is
  * 0 everywhere, p takes its place; where p is too, next is -1.  Negative and NaN probabilities count as 0.
+ * A sum R over a whole row is formed only where a drawn sibling is tried after a rejection, and then by every
+ * workgroup of the sequence (about 10 us for 151936 tokens; more with each rejection before it).
  * Formed in fp64 from fp32 inputs, so a choice depends on the order of sums only where u0 times the sum meets
  * a partial sum to about 1e-15.
  *   target:  fp32 [n_rows, vocab]: probabilities after each row, target_row_stride ELEMENTS from one row to
@@ -120,7 +122,7 @@ int delta_verify_drafts(int32_t batch, int32_t n_rows, int32_t max_new, const in
  * rows of token P + path[b, i] move to token P + i, i < n_path[b], in every KV head, bit for bit.
  *   kv:       HOST array of n_layers descriptors; the caches are written in place.  kv_type may differ from
  *             layer to layer, and page_table too; seq_lens is one for all (else DELTA_ERR_INVALID_ARG) and
- *             counts the runs.
+ *             counts the runs.  All caches are different ones (else DELTA_ERR_INVALID_ARG).
  *   path, n_path: as delta_verify_drafts writes them: path int32 [batch, max_new]
  *   max_new:  at least 1 and at most n_rows
  *   new_lens: int32 [batch]: P + n_path[b]; may be the layers' seq_lens; NULL: not written.

@@ -238,6 +238,11 @@ int delta_cache_compact(const delta_shape_t* shape, int32_t n_layers, const delt
     if ((rc = check_kv(kv + i))) return rc;
     if (kv[i].seq_lens != kv[0].seq_lens || !aligned(kv[i].k_cache, 16) || !aligned(kv[i].v_cache, 16))
       return DELTA_ERR_INVALID_ARG;
+    // (a cache that is named twice would be moved twice at once)
+    if (kv[i].k_cache == kv[i].v_cache) return DELTA_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      for (const void* p : {kv[i].k_cache, kv[i].v_cache})
+        if (p == kv[j].k_cache || p == kv[j].v_cache) return DELTA_ERR_INVALID_ARG;
   }
   if ((rc = check_drafts(shape->batch, n_rows, max_new, row_offsets))) return rc;
   if (max_new < 1 || !path || !n_path) return DELTA_ERR_INVALID_ARG;

@@ -156,7 +156,12 @@ def alloc_verify_workspace(batch, vocab, device="cuda") -> torch.Tensor:
 
 
 def _probabilities(name, t, rows):
-    """A float32 [rows, vocab] GPU tensor whose rows may stand apart; its row stride."""
+    """A float32 [rows, vocab] GPU tensor whose rows may stand apart; its row stride.  What passes is found out
+    first, and what does not is given its message after."""
+    if type(t) is torch.Tensor and t.is_cuda and t.dtype == torch.float32:
+        have, stride = t.shape, t.stride()
+        if len(have) == 2 and stride[1] == 1 and (rows is None or have == rows):
+            return stride[0] if have[0] > 1 else have[1]   # (the stride of a single row says nothing)
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
     if not t.is_cuda:

@@ -19,7 +19,7 @@ def shape(**kw):
     return D.make_shape(**s)
 
 
-def cache(k=0x1000, v=0x1000, table=0x1000, lens=0x1000, n_pages=0, kv_type=0):
+def cache(k=0x1000, v=0x2000, table=0x1000, lens=0x1000, n_pages=0, kv_type=0):
     return D.delta_kv_t(k, v, table, lens, n_pages, kv_type)
 
 
@@ -129,15 +129,16 @@ def test_verification_workspace():
 
 
 def compact(s=None, kvs=None, n_layers=None, n_rows=9, max_new=4, offsets=FAKE, path=FAKE, n_path=FAKE, lens=None):
-    kvs = kvs or [cache(), cache(kv_type=1)]
+    kvs = kvs or [cache(), cache(0x3000, 0x4000, kv_type=1)]
     arr = (D.delta_kv_t * len(kvs))(*kvs)
     return D._lib.delta_cache_compact(ctypes.byref(s or shape()), len(kvs) if n_layers is None else n_layers, arr, n_rows,
                                       max_new, offsets, path, n_path, lens, None)
 
 
 @pytest.mark.parametrize("kw,rc", [
-    (dict(n_layers=0), -1), (dict(kvs=[cache(), cache(lens=0x2000)]), -1), (dict(kvs=[cache(k=0x1008)]), -1),
-    (dict(kvs=[cache(), cache(v=None)]), -1), (dict(n_rows=-1), -1), (dict(max_new=0), -1), (dict(max_new=10), -1),
+    (dict(n_layers=0), -1), (dict(kvs=[cache(), cache(0x3000, 0x4000, lens=0x2000)]), -1), (dict(kvs=[cache(k=0x1008)]), -1),
+    (dict(kvs=[cache(), cache(0x3000, None)]), -1), (dict(kvs=[cache(v=0x1000)]), -1), (dict(kvs=[cache(), cache(0x3000)]), -1),
+    (dict(kvs=[cache(), cache(0x2000, 0x3000)]), -1), (dict(n_rows=-1), -1), (dict(max_new=0), -1), (dict(max_new=10), -1),
     (dict(offsets=None), -1), (dict(path=None), -1), (dict(n_path=None), -1), (dict(s=shape(head_dim=80)), -2),
     (dict(n_rows=600, max_new=513), -2),
 ])
