@@ -7,8 +7,7 @@
 // "Online normalizer calculation for softmax", 2018).
 //
 // Work.  The rows of a run that share a KV head (token-major, the group's query heads next to each
-// other) are cut into tiles; a workgroup takes a tile, and one of n_split pieces of the keys that
-// the tile's last row sees.  A wave holds 32 rows and takes 32*KT keys of a block; WR waves stand
+// other) are cut into tiles; a workgroup takes a tile, and a piece of the keys that it sees.  A wave holds 32 rows and takes 32*KT keys of a block; WR waves stand
 // along the rows, WK along the keys.
 //
 // Per 32 keys and wave:

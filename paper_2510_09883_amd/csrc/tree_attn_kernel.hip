@@ -10,16 +10,29 @@
 // shares of the tiles' blocks of keys, found from the lengths on the device (make_cut).  A tile whose blocks fall
 // to several groups leaves parts (two at most per workgroup: its first and its last tile), which a second
 // launch joins.
-// A tile is taken by eight waves in the form that its rows fill: (waves along the rows) x (along the keys) is 1 x 8
-// up to 32 rows, 2 x 4 up to 64, 4 x 2 up to 128, 8 x 1 above; calls without longer runs than 32 rows have
-// workgroups of four waves, 1 x 4, two on a CU.
+//   * tiles of 256 rows: eight waves, one workgroup a CU.  Up to 128 rows the waves stand 4 x 2 (along the rows x along
+//     the keys), above 8 x 1.  Blocks come through a ring in LDS (attend_runs.h); only e4m3 blocks of up to 128 rows
+//     wait in registers and are twice as long, which leaves the waves more products between two barriers (32/8 heads,
+//     16 sequences of 4K-16K, 32 rows each: 151 us, through the ring 163; bf16 by registers 183, through the ring 175).
+//   * tiles of 32 rows (no longer run, or little to walk): four waves along the keys, each with keys of its own.
+//
+// Bound.  256 rows: the card's power, then issue, as for causal runs: 16 trees of 64 nodes behind 4K-16K tokens, 32/8
+// heads, 217 us at 2.03 GHz (807 TFLOP/s, VALU 50 % and MFMA 40 % of the SIMDs' cycles) and 12 us for the join, which reads
+// 50 MB of parts; taking the loads out leaves 164 us together, taking the products out 154.
+// 33 to 128 rows of bf16: HBM, 16 of 4K-16K with 16 nodes 146 us together (4.8 TB/s); of e4m3: phases that follow one
+// another between the barriers (loads, conversion, products, softmax; VALU 34 %, LDS 30 %, MFMA 24 %), 12 of 10K-32K with
+// 8 to 24 nodes, 40/8 heads, 156 us and 6.5 for the join.  Measured slower or equal there: tiles of 128 rows by four waves,
+// two workgroups a CU (bf16 -8 % to +2 %, e4m3 +17 % to +25 %), e4m3 blocks through a ring of two (+0 to +4 %).
+// Few rows: 16 of 4K-16K with 8 nodes 131 us together (5.4 TB/s); with a row of units per head instead of groups that
+// walk the same pages at the same time 138.  One tree of 16 behind 8192 tokens, 28/4 heads: 14.6 and 3.2 for the join, of
+// which about 9 are there with one block, for the chain offsets -> queries, masks and pages -> blocks.
 #include "attend_runs.h"
 #include "drafts.h"
 
 namespace delta {
 namespace {
 
-// Keys of a block and its units for tiles of so many rows (the times of the bodies on a CU, relative).
+// Keys of a block and its units for tiles of so many rows: what a CU takes for it while all are busy, in about 0.14 us.
 struct Form {
   int keys, units;
 };
