@@ -7,8 +7,8 @@
 // "Online normalizer calculation for softmax", 2018).
 //
 // Work.  The rows of a run that share a KV head (token-major, the group's query heads next to each
-// other) are cut into tiles; a workgroup takes a tile, and a piece of the keys that it sees.  A wave holds 32 rows and takes 32*KT keys of a block; WR waves stand
-// along the rows, WK along the keys.
+// other) are cut into tiles; a workgroup takes a tile, and a piece of the keys that it sees.  A
+// wave holds 32 rows and takes 32*KT keys of a block; WR waves stand along the rows, WK along the keys.
 //
 // Per 32 keys and wave:
 //   * S^T = K Q^T by v_mfma_f32_32x32x16_bf16 with A = 32 keys, B = the 32 rows' queries (in

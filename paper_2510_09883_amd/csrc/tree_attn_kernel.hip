@@ -16,16 +16,17 @@
 //     16 sequences of 4K-16K, 32 rows each: 151 us, through the ring 163; bf16 by registers 183, through the ring 175).
 //   * tiles of 32 rows (no longer run, or little to walk): four waves along the keys, each with keys of its own.
 //
-// Bound.  256 rows: the card's power, then issue, as for causal runs: 16 trees of 64 nodes behind 4K-16K tokens, 32/8
-// heads, 217 us at 2.03 GHz (807 TFLOP/s, VALU 50 % and MFMA 40 % of the SIMDs' cycles) and 12 us for the join, which reads
-// 50 MB of parts; taking the loads out leaves 164 us together, taking the products out 154.
+// Bound.  256 rows: issue, at the lower clock that loads and products together leave: 16 trees of 64 nodes behind 4K-16K
+// tokens, 32/8 heads, 217 us at 2.03 GHz (834 TFLOP/s, VALU 50 % and MFMA 40 % of the SIMDs' cycles) and 12 us for the
+// join, which reads 48 MB of parts.  In an earlier state, 232 us together, taking the loads out left 164, taking the
+// products out 154.
 // 33 to 128 rows of bf16: HBM, 16 of 4K-16K with 16 nodes 146 us together (4.8 TB/s); of e4m3: phases that follow one
-// another between the barriers (loads, conversion, products, softmax; VALU 34 %, LDS 30 %, MFMA 24 %), 12 of 10K-32K with
+// another between the barriers (loads, conversion, products, softmax; VALU 33 %, LDS 30 %, MFMA 24 %), 12 of 10K-32K with
 // 8 to 24 nodes, 40/8 heads, 156 us and 6.5 for the join.  Measured slower or equal there: tiles of 128 rows by four waves,
-// two workgroups a CU (bf16 -8 % to +2 %, e4m3 +17 % to +25 %), e4m3 blocks through a ring of two (+0 to +4 %).
+// two workgroups a CU (bf16 -9 % to +3 %, e4m3 +18 % to +26 %), e4m3 blocks through a ring of two (+1 % to +4 %).
 // Few rows: 16 of 4K-16K with 8 nodes 131 us together (5.4 TB/s); with a row of units per head instead of groups that
-// walk the same pages at the same time 138.  One tree of 16 behind 8192 tokens, 28/4 heads: 14.6 and 3.2 for the join, of
-// which about 9 are there with one block, for the chain offsets -> queries, masks and pages -> blocks.
+// walk the same pages at the same time 138.  One tree of 16 behind 8192 tokens, 28/4 heads: 14.6 and 3.2 for the join;
+// behind 64 tokens, in one launch, 7.1 in a graph: the chain offsets -> queries, masks and pages -> blocks.
 #include "attend_runs.h"
 #include "drafts.h"
 

@@ -17,9 +17,10 @@
 //
 // Bound: latencies, of launches and of the chains offsets -> parents -> values -> row and sums -> row (one tree of 16
 // chosen drafts, 151936 tokens: 5.3 us and 3.7); then the reads of the rows (64 chains of drawn drafts, 78 MB: 17 us, 4.6
-// TB/s, and 4.5).  Measured slower there: the last of a sequence's workgroups to arrive at a counter picks the token
-// (38 us together; with release and acquire at the counter 140 to 330), finding the token by LDS atomics of all
-// threads on one word (6 us more), a wave's rounds of 4 bytes a lane (31 us together).
+// TB/s, and 4.5).  Measured for the chains, both launches in a graph: finding the token by LDS atomics of all threads on
+// one word 38 us, by ballots 31; with parts that are whole rounds of 16 bytes a lane, where nearly half of a part was
+// read 4 bytes a lane before, 25.  That the last of a sequence's workgroups to arrive at a counter picks the token was
+// no faster than a second launch (38 us for both), and 208 with release and acquire at the counter.
 #include <algorithm>
 
 #include "drafts.h"
