@@ -31,6 +31,7 @@
 
 #include <algorithm>
 
+#include "attend_lds.h"
 #include "attn_tile.h"
 #include "debug_check.h"
 #include "runs.h"
@@ -132,15 +133,6 @@ __device__ __forceinline__ int held(int x) {
 constexpr int kMostMaskWords = 16;
 template <int ROWS>
 constexpr int kMaskLds = (ROWS + 2) * kMostMaskWords;
-
-// Blocks that a ring holds, and the pages that it looks up at a time.
-constexpr int kRing = 4, kRingPages = 1024;
-
-// LDS of a body, in bytes: K and V of the blocks, later the outputs of the waves along the keys.
-template <int D, int WR, int WK, int KT, bool RING = false, bool KV8 = false>
-constexpr int kBodyLds = std::max(RING ? (KV8 ? 2 * 2 * 2 + kRing * 2 : kRing * 2 * 2) * 32 * KT * WK * D
-                                       : 2 * (WR == 1 ? 1 : 2) * 32 * KT * WK * D * 2,
-                                  WK > 1 ? WR * WK * 64 * D / 2 * 4 : 0);
 
 // Loads 16 bytes a lane to LDS, lane after lane from byte `lds` on, past the registers.  Nothing but load_wait waits
 // for it.
@@ -459,7 +451,7 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   if constexpr (RING) {
     const uint32_t s_kv_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)s_kv;
     constexpr int kLoads = 2 * NL;                           // of a wave and block
-    constexpr int kRaw = KV8 ? 4 * kBlock * 2 : 0;           // e4m3: where the waves' own LDS begins, in bytes
+    typedef RawRing<D, NW, BN> Raw;                          // e4m3: the waves' own LDS
     // a lane's 16 bytes of the rows of a load; bf16: that which stands in its place of the permuted rows (the
     // rows of a wave's loads lie a multiple of 16 apart, or of what else the permutation knows of a row)
     const int lr = lane / CPR, lc = lane % CPR;
@@ -485,7 +477,7 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
         // (in vector registers: scalar ones are short)
         const uint32_t page = s_pages[min(blk * (BN / 16) + row / 16, last_page) - base_page];
         const size_t at = ((size_t)page * (uint32_t)a.page_stride + (uint32_t)((g * 16 + row % 16) * D)) * EB;
-        const uint32_t to = s_kv_at + (KV8 ? kRaw + ((wave * kRing + stage) * NL + i) * 2048
+        const uint32_t to = s_kv_at + (KV8 ? Raw::at(wave, stage, i)
                                            : (stage * 2 * kBlock + row * D) * 2);
         load_to_lds(a.k_cache + at + k_lane, to);
         load_to_lds(a.v_cache + at + v_lane, to + (KV8 ? 1024 : kBlock * 2));
@@ -501,14 +493,15 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
     };
     if (blk0 < blk1) {
       if constexpr (KV8) {
-        const u32x4* raw = reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(s_kv) + kRaw + wave * kRing * NL * 2048 + lane16);
         auto convert = [&](int blk) {
           arrived(min(kRing - 1, blk1 - 1 - blk));
           const int stage = (blk - blk0) % kRing;
 #pragma unroll
           for (int i = 0; i < NL; ++i) {
-            kr[i] = raw[(stage * NL + i) * 128];
-            vr[i] = raw[(stage * NL + i) * 128 + 64];
+            if (kPieces % T && !Raw::has(wave, i)) break;
+            const uint8_t* raw = reinterpret_cast<const uint8_t*>(s_kv) + Raw::at(wave, stage, i) + lane16;
+            kr[i] = *reinterpret_cast<const u32x4*>(raw);
+            vr[i] = *reinterpret_cast<const u32x4*>(raw + 1024);
           }
           store(blk, (blk - blk0) & 1);
           wave_lds_sync();   // (its own LDS has been read)
