@@ -200,8 +200,9 @@ def delta_verify_drafts(target, draft, tokens, parents, uniform, row_offsets, pa
 
 
 class CacheStack:
-    """The cache descriptors of a model's layers, for calls that work on all of them at once: checked and
-    built once, reused every round.  All share seq_lens."""
+    """The cache descriptors of a model's layers, for calls that work on all of them at once: built once, reused
+    every round.  All share seq_lens.  As with a single descriptor, every call looks whether the tensors are
+    still what make_kv was given."""
 
     def __init__(self, shape, kvs):
         if not kvs:
@@ -213,12 +214,31 @@ class CacheStack:
                 raise ValueError(f"a layer's cache is on {mine[0].device}, the first one's on {first[0].device}")
         self.shape, self.n, self.layers = shape, len(kvs), list(kvs)
         self.kvs = (delta_kv_t * self.n)(*kvs)
+        self._sizes = _sizes(shape)
+        # every tensor once, as tables and lengths are often those of all layers (scales are not read)
+        made = {id(x): (x, *m) for kv in kvs if hasattr(kv, "_tensors") for x, m in zip(kv._tensors, kv._made)}
+        self._tensors, self._shapes, self._places = map(list, zip(*made.values())) if made else ([], [], [])
+
+    def _check(self):
+        """All tensors at once (28 layers: 11 us; one descriptor after the other 31); what has changed finds
+        its message after."""
+        one = torch.Tensor
+        if (self._sizes != _sizes(self.shape) or list(map(one.data_ptr, self._tensors)) != self._places
+                or list(map(one.size, self._tensors)) != self._shapes
+                or False in map(one.is_contiguous, self._tensors)):
+            for kv in self.layers:
+                _check_kv(kv, self.shape)
+
+
+def _sizes(shape):
+    return shape.n_kv_heads, shape.page_size, shape.head_dim, shape.batch, shape.max_pages_per_seq
 
 
 def delta_cache_compact(stack: CacheStack, n_rows, row_offsets, path, n_path, new_lens=None):
     """Moves the accepted rows path [batch, max_new], n_path [batch] of every run together in the caches of
     all layers; new_lens [batch] (None: not written) gets the lengths, and may be the layers' seq_lens."""
     shape = stack.shape
+    stack._check()
     _dev("path", path, torch.int32, (shape.batch, None))
     _dev("n_path", n_path, torch.int32, (shape.batch,))
     if new_lens is not None:
