@@ -69,10 +69,13 @@ int delta_tree_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int32
  *               from the run's length on are ignored.  A row sees itself only if its own bit is set.
  *   mask_words: >= 1 and at least max_new / 32, rounded up
  *   q, out, max_new, ws, and what is undefined with a run longer than max_new: as in delta_extend_attn, so
- *   also the precision (probabilities rounded to bf16 before they meet the values), infinite and NaN keys
- *   and values (a row gets them of the tokens that it sees, and no others), max_seq_len, which decides the
- *   speed of calls of few rows, and determinism.  Calls of more than 65535 tiles (as counted there) give
- *   DELTA_ERR_UNSUPPORTED. */
+ *   also infinite and NaN keys and values (a row gets them of the tokens that it sees, and no others),
+ *   max_seq_len, which decides the speed of calls of few rows, and determinism.  Calls of more than 65535 tiles
+ *   (as counted there) give DELTA_ERR_UNSUPPORTED.
+ * bf16 queries, fp32 scores, softmax and sums, one bf16 rounding of the result.  Where they meet the values
+ * (their sum is not rounded) the probabilities have 16 bits: over e4m3 caches those of fp16 (at most 2^-11 of
+ * each); over bf16 caches two bf16 terms (2^-16) where runs have up to 32 rows a KV head (max_new * G, G query
+ * heads per KV head) or the batch has little to walk, else one (2^-8). */
 int delta_tree_attn(const delta_shape_t* shape, const delta_kv_t* kv, int32_t n_rows, int32_t max_new,
                     const int32_t* row_offsets, const uint32_t* masks, int32_t mask_words, const void* q,
                     void* out, void* ws, size_t ws_bytes, void* stream);

@@ -25,8 +25,14 @@
 // 16 rows touch all banks), V rows with their 64-byte pieces permuted by the row (the four rows of
 // a transposing read do).  The counters show no bank conflict.
 //
-// Precision.  Scores, maximum, sum and outputs are fp32; a probability is rounded to bf16 for the
-// P V product, whose inputs the matrix cores take in 16 bits (at most 2^-8 of each).
+// Precision.  Scores, maximum, sum and outputs are fp32.  The matrix cores take the inputs of the P V product in 16
+// bits, so there a probability is rounded:
+//   * causal runs, and trees in tiles of 256 rows of bf16 caches: to bf16, at most 2^-8 of each (see
+//     tree_attn_kernel.hip for the price of a second term);
+//   * trees in tiles of 32 rows of bf16 caches: to two bf16 terms, 2^-16 of each (kTwoTerms), which costs little
+//     where the cache's bytes or a chain of loads decide;
+//   * trees over e4m3 caches: to fp16, 2^-11 of each (kHalf).  fp16 holds every e4m3 value, and the conversions and
+//     products of both types take the same time.
 #pragma once
 
 #include <algorithm>
@@ -40,6 +46,8 @@ namespace delta {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
@@ -149,6 +157,13 @@ __device__ __forceinline__ void load_wait() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+// Two e4m3 values, in the lower or the upper half of a word, as fp16 or bf16.
+template <bool HALF, bool HI>
+__device__ __forceinline__ uint32_t e4m3x2_to(uint32_t w) {
+  if (HALF) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, HI));
+  return e4m3x2_to_bf16x2<HI>(w);
+}
+
 // What a row sees.  Causal runs: the tokens up to itself.  TREE: the tokens before the run, and of the
 // run's rows those whose bits are set in the row's mask.
 //
@@ -186,6 +201,16 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
   // barriers, and needs one buffer of it.
   constexpr bool kOwnKeys = WR == 1;
   constexpr int kBuffers = kOwnKeys ? 1 : 2;
+  // the inputs of the P V product (see Precision)
+  constexpr bool kHalf = TREE && KV8, kTwoTerms = TREE && !KV8 && WR == 1;
+  // (fp16 probabilities stand for 2^15 times as much, in the sums as well, so that those from 2^-29 on are normal)
+  constexpr float kLift = kHalf ? 15.f : 0.f;
+  auto add_values = [&](const bf16x8& v, const u32x4& p, const f32x16& c) {
+    if constexpr (kHalf)
+      return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, p), c, 0, 0, 0);
+    else
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, p), c, 0, 0, 0);
+  };
   constexpr int kBlock = BN * D;        // elements of a K or V block
   const int b = t.b, n_new = t.n_new, s_b = t.s_b, n_tile_rows = t.n_rows, begin = t.begin;
   // this lane's row: token j of the run, query head g * G + head
@@ -318,8 +343,8 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
           for (int w = 0; w < 2; ++w) {
             wk[2 * w] = e4m3x2_to_bf16x2<false>(kr[i][2 * half + w]);
             wk[2 * w + 1] = e4m3x2_to_bf16x2<true>(kr[i][2 * half + w]);
-            wv[2 * w] = e4m3x2_to_bf16x2<false>(vr[i][2 * half + w]);
-            wv[2 * w + 1] = e4m3x2_to_bf16x2<true>(vr[i][2 * half + w]);
+            wv[2 * w] = e4m3x2_to<kHalf, false>(vr[i][2 * half + w]);
+            wv[2 * w + 1] = e4m3x2_to<kHalf, true>(vr[i][2 * half + w]);
           }
           *reinterpret_cast<u32x4*>(sk + k_at<D>(row, 2 * c + half)) = wk;
           *reinterpret_cast<u32x4*>(sv + v_at<D>(row, 16 * c + 8 * half)) = wv;
@@ -411,7 +436,7 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[d] *= alpha;
       }
-      const float m_use = m == kNegInfF ? 0.f : m;
+      const float m_use = (m == kNegInfF ? 0.f : m) - kLift;
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -424,25 +449,35 @@ __device__ __forceinline__ void extend_body(const ExtendArgs& a, const TileOf& t
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        u32x4 pw;
+        u32x4 pw, rest;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const bf16x2 p = {(__bf16)s[kt][8 * st + 2 * w], (__bf16)s[kt][8 * st + 2 * w + 1]};
-          pw[w] = __builtin_bit_cast(uint32_t, p);
+          const float p0 = s[kt][8 * st + 2 * w], p1 = s[kt][8 * st + 2 * w + 1];
+          if constexpr (kHalf) {
+            pw[w] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)p0, (_Float16)p1});
+          } else {
+            pw[w] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p0, (__bf16)p1});
+            if constexpr (kTwoTerms)
+              rest[w] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(p0 - __uint_as_float(pw[w] << 16)),
+                                                            (__bf16)(p1 - __uint_as_float(pw[w] & 0xffff0000u))});
+          }
         }
-        const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
         if constexpr (kGrouped) {
 #pragma unroll
           for (int d = 0; d < ND; ++d) read(v_part[st][d]);
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_part[st][d], pb, o[d], 0, 0, 0);
+            o[d] = add_values(v_part[st][d], pw, o[d]);
             if (kt + 1 < KT) v_part[st][d] = value_part(2 * (kt + 1) + st, d);
           }
         } else {
+          bf16x8 v[ND];
 #pragma unroll
-          for (int d = 0; d < ND; ++d)
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_part(2 * kt + st, d), pb, o[d], 0, 0, 0);
+          for (int d = 0; d < ND; ++d) o[d] = add_values(v[d] = value_part(2 * kt + st, d), pw, o[d]);
+          if constexpr (kTwoTerms) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d) o[d] = add_values(v[d], rest, o[d]);
+          }
         }
       }
   };

@@ -16,6 +16,14 @@
 //     16 sequences of 4K-16K, 32 rows each: 151 us, through the ring 163; bf16 by registers 183, through the ring 175).
 //   * tiles of 32 rows (no longer run, or little to walk): four waves along the keys, each with keys of its own.
 //
+// Precision.  A probability meets the values in 16 bits (attend_runs.h).  Two bf16 terms for each, what the first leaves
+// as well, cost tiles of 32 rows little, us without and with them: 16 sequences of 4K-16K tokens, 8 nodes, 32/8 heads 131
+// and 132, 32 short ones 10.1 and 9.9, one tree of 16 behind 8192 tokens, 28/4 heads, 19.8 and 20.5, one of 64 behind 2048
+// 20.3 and 21.5.  Tiles of 256 rows would pay for them (16 sequences of 4K-16K, 32/8 heads, 16 nodes 147 and 169, 32
+// nodes 178 and 209, 64 of each 238 and 300) and keep the one: 1.69e-3 rms off float64 instead of the output's own
+// rounding's 1.66e-3.  e4m3 caches: two bf16 terms took 284 where one takes 168 (12 trees of 8 to 24 nodes, 40/8 heads),
+// fp16 169.
+//
 // Bound.  256 rows: issue, at the lower clock that loads and products together leave: 16 trees of 64 nodes behind 4K-16K
 // tokens, 32/8 heads, 217 us at 2.03 GHz (834 TFLOP/s, VALU 50 % and MFMA 40 % of the SIMDs' cycles) and 12 us for the
 // join, which reads 48 MB of parts.  In an earlier state, 232 us together, taking the loads out left 164, taking the

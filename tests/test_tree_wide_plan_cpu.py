@@ -63,6 +63,11 @@ def test_the_other_cases_too(exe):
     assert plan.rows == 256 and not plan.workgroups    # a workgroup walks its tile's whole sequence
 
 
+def test_the_cases_of_small_tiles_take_them(exe):
+    calls = [C.plan_call((lens, new, G * hkv, hkv, None)) for lens, new in C.SMALL_TILES for G, hkv in C.SMALL_HEADS]
+    assert {p.rows for p in P.ask(exe, calls)} == {32}
+
+
 def test_shapes_of_the_cases_are_taken():
     from paper_2510_09883_amd import delta as D
     from paper_2510_09883_amd import drafts as T

@@ -53,6 +53,11 @@ SHARP = ((900, 1300), (90, 200), 32, 8, None)
 BITS = ((1000, 300, 90, 33), (70, 100, 40, 33), 32, 8, None)
 NOTHING = ((1000, 90, 64, 0), (100, 90, 64, 5), 32, 8, None)
 
+# Calls that take tiles of 32 rows, whatever the number of heads (query heads a group, KV heads)
+SMALL_TILES = [((3, 8, 20, 41), (3, 4, 4, 2)), ((150, 700, 64, 1), (4, 2, 3, 1)), ((40, 300, 90), (40, 33, 64)),
+               ((2600, 1900), (4, 3)), ((9000,), (4,))]
+SMALL_HEADS = [(1, 4), (4, 2), (7, 1)]
+
 # ... of one workgroup that walks more pages than it looks up at a time: more sequences than are shared out
 PAGES = ((16500, 35000, 17000), (70, 20, 9))
 
@@ -93,11 +98,12 @@ def plan_call(case, pad=0, more=0):
     return len(lens), hq, hkv, bound or max(lens), sum(new) + pad, max(new) + more
 
 
-def attend_runs(call, k_of=None, v_of=None):
+def attend_runs(call, k_of=None, v_of=None, p_round=None):
     """float64 outputs [rows, hq, d] of all rows of the runs of a test_gpu_tree_attn.Call, and how far a
     device result may be off: the bound of cache_cases.attend, row by row, with the values' largest of all
     the sequence's.  k_of, v_of: a sequence's keys and values instead of the cache's."""
     c, outs, tols = call, [], []
+    p_round = P_ROUND if p_round is None else p_round
     hkv, d = c.cache.hkv, c.q.shape[2]
     G, row = c.hq // hkv, 0
     for b, (s, n) in enumerate(zip(c.lens, c.new)):
@@ -117,7 +123,7 @@ def attend_runs(call, k_of=None, v_of=None):
                 e = (q.abs() @ k[:, h].abs().t().contiguous() * c.scale).masked_fill(hidden, 0).amax(1, keepdim=True)
                 p = torch.where(some, torch.softmax(x, -1), 0.0)
                 o = p @ v[:, h].contiguous()
-                t = P_ROUND * (p @ v[:, h].abs().contiguous()) + o.abs() * 2.0 ** -8
+                t = p_round * (p @ v[:, h].abs().contiguous()) + o.abs() * 2.0 ** -8
                 t += 2 * (e * (d + 4) * 2.0 ** -24 + 2.0 ** -22 + s * 2.0 ** -24) * v[:, h].abs().max()
                 out[:, h * G:(h + 1) * G] = o.view(n, G, d)
                 tol[:, h * G:(h + 1) * G] = torch.where(some, t, 0.0).view(n, G, d)
