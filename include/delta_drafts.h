@@ -98,7 +98,7 @@ int delta_verify_workspace_bytes(int32_t batch, int32_t vocab, size_t* out);
  * u0 the uniform number of the run's first row (the last token with r > 0 if there is no such v).  Where r is
  * 0 everywhere, p takes its place; where p is too, next is -1.  Negative and NaN probabilities count as 0.
  * A sum R over a whole row is formed only where a drawn sibling is tried after a rejection, and then by every
- * workgroup of the sequence (about 10 us for 151936 tokens; more with each rejection before it).
+ * workgroup of the sequence (13 us for 151936 tokens).
  * Formed in fp64 from fp32 inputs, so a choice depends on the order of sums only where u0 times the sum meets
  * a partial sum to about 1e-15.
  *   target:  fp32 [n_rows, vocab]: probabilities after each row, target_row_stride ELEMENTS from one row to

@@ -44,7 +44,7 @@ constexpr int kMostVocab = kMostPieces * kMostPiece;
 // A sequence's part of the workspace, from the first launch to the second.
 struct VerifyState {
   int32_t cur, k;                            // the last accepted row and the rejections at it
-  double left[kMostDrafts];                  // R before each of them, of drawn drafts
+  double S;                                  // the sum of R before each of them, of drawn drafts
   double sums[kMostPieces * kVerifyWaves];   // a part's sum of r
 };
 

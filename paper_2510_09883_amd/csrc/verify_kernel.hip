@@ -62,13 +62,11 @@ struct Shared {
   int16_t parent[kMostDrafts];     // -1: never tried
   int32_t token[kMostDrafts];
   float uniform[kMostDrafts], p[kMostDrafts], q[kMostDrafts];
-  double left[kMostDrafts];        // R before each rejection at the current row
   double wave[kWaves];
   uint32_t dropped[kMostPiece / 32];   // tokens of the piece that were rejected (draft == null)
 };
 
 struct SharedPick {
-  double left[kMostDrafts];
   double wave[kWaves], before;
   double part[kMostPieces * kWaves];   // sums of p, where they are needed
   uint32_t dropped[kMostPiece / 32];
@@ -157,13 +155,9 @@ __device__ __forceinline__ void for_row(const float* p, const float* q, int firs
 // A probability; negative and NaN ones count as 0.
 __device__ __forceinline__ double mass_of(float x) { return fmaxf(x, 0.f); }
 
-// r after k rejections of drawn drafts.
-__device__ __forceinline__ double residual(float p, float q, int k, const double* left) {
-  double r = mass_of(p);
-  if (k) r = fmax(r - mass_of(q), 0.0);   // (left[0] is 1)
-  for (int i = 1; i < k; ++i) r = fmax(r - left[i] * mass_of(q), 0.0);
-  return r;
-}
+// r after rejections of drawn drafts, S the sum of R before each of them: as q and R are not negative,
+// max(max(p - R0 q, 0) - R1 q, 0) = max(p - (R0 + R1) q, 0), and so on.
+__device__ __forceinline__ double residual(float p, float q, double S) { return fmax(mass_of(p) - S * mass_of(q), 0.0); }
 
 // The current row's probabilities after k rejections, in pieces and waves' parts of them.
 struct Row {
@@ -171,13 +165,13 @@ struct Row {
   int vocab, part, per;        // elements of a part and of a piece
   int k;
   bool drawn;
-  const double* left;          // LDS
+  double S;                    // of drawn drafts: see residual
   uint32_t* dropped;           // LDS: rejected tokens of a piece, if they were not drawn
 
-  __device__ __forceinline__ Row(const VerifyArgs& a, int begin, int cur, int k, const double* left, uint32_t* dropped)
+  __device__ __forceinline__ Row(const VerifyArgs& a, int begin, int cur, int k, double S, uint32_t* dropped)
       : p(a.target + (int64_t)(begin + cur) * a.target_stride),
         q(a.draft && k ? a.draft + (int64_t)(begin + cur) * a.draft_stride : nullptr),
-        vocab(a.vocab), k(k), drawn(a.draft != nullptr), left(left), dropped(dropped) {
+        vocab(a.vocab), k(k), drawn(a.draft != nullptr), S(S), dropped(dropped) {
     part = a.part;
     per = part * kWaves;
   }
@@ -199,7 +193,7 @@ struct Row {
   }
   // r of element v of the piece from v0 on
   __device__ __forceinline__ double r_of(int v, float x, float y, int v0) const {
-    if (drawn) return residual(x, y, k, left);
+    if (drawn) return residual(x, y, S);
     return k && (dropped[(v - v0) >> 5] >> ((v - v0) & 31) & 1) ? 0.0 : mass_of(x);
   }
 };
@@ -235,20 +229,16 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
   // ---- the way through the tree, the same in all threads
   int cur = 0, count = 1;
   int k = 0;              // rejections at the current row
-  int summed = 0;         // of them, those with R known: s.left[0 .. summed] holds R before each and after
-  double left = 1.0;      // R, where draft is null
-  if (tid == 0) s.left[0] = 1.0;
+  double R = 1.0, S = 0.0;   // r's sum, and of drawn drafts the sum of R before each rejection
+  bool known = true;         // (R is formed when a test needs it)
   if (piece == 0 && tid == 0) path[0] = 0;
-  __syncthreads();
-  auto sum_left = [&]() {   // R after rejection summed + 1, over the whole row
+  auto sum_row = [&]() {     // R, over the whole row
     const float* p = target + (int64_t)cur * a.target_stride;
     const float* q = draft + (int64_t)cur * a.draft_stride;
     double sum = 0;
-    for_row<kThreads>(p, q, 0, a.vocab, tid, [&](int, float x, float y) { sum += residual(x, y, summed + 1, s.left); });
-    sum = block_sum(sum, s.wave);
-    ++summed;
-    if (tid == 0) s.left[summed] = sum;
-    __syncthreads();
+    for_row<kThreads>(p, q, 0, a.vocab, tid, [&](int, float x, float y) { sum += residual(x, y, S); });
+    R = block_sum(sum, s.wave);
+    known = true;
   };
   for (int c0 = 0; c0 < n; c0 += 64) {
     const int parent = c0 + lane < n ? s.parent[c0 + lane] : -1;
@@ -256,43 +246,45 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
     while (children) {
       const int at = __builtin_ctzll(children), j = c0 + at;
       const int x = s.token[j];
-      double r, mass;
+      double r;
       if (draft) {
-        while (summed < k) sum_left();
-        r = residual(s.p[j], s.q[j], k, s.left);
-        mass = s.left[k];
+        if (!known) sum_row();
+        r = residual(s.p[j], s.q[j], S);
       } else {
         r = mass_of(s.p[j]);
-        mass = left;
         bool again = false;   // a sibling with this token has been rejected
         if (k)
           for (int c = cur & ~63; c <= c0; c += 64)
             again |= __any(c + lane < j && s.parent[c + lane] == cur && s.token[c + lane] == x);
         if (again) r = 0;
       }
-      if ((double)s.uniform[j] * (double)s.q[j] * mass < r) {
+      if ((double)s.uniform[j] * (double)s.q[j] * R < r) {
         if (piece == 0 && tid == 0) path[count] = j;
         cur = j;
         ++count;
-        k = summed = 0;
-        left = 1.0;
+        k = 0;
+        R = 1.0, S = 0.0;
+        known = true;
         children = __ballot(parent == cur) & ~((2ull << at) - 1);
       } else {
         ++k;
-        if (!draft) left = fmax(left - r, 0.0);
+        if (draft) {
+          S += R;
+          known = false;
+        } else {
+          R = fmax(R - r, 0.0);
+        }
         children &= children - 1;
       }
     }
   }
-  if (draft)
-    while (summed < k - 1) sum_left();
   if (piece == 0) {
     for (int i = count + tid; i < a.max_new; i += kThreads) path[i] = -1;
     if (tid == 0) a.n_path[b] = count;
   }
 
   // ---- the sum of r over this workgroup's piece, a part of it by each wave
-  const Row row(a, begin, cur, k, s.left, s.dropped);
+  const Row row(a, begin, cur, k, S, s.dropped);
   const int v0 = piece * row.per, mine = piece * kWaves + (tid >> 6);
   row.mark_dropped(v0, cur, n, [&](int j) { return (int)s.parent[j]; }, [&](int j) { return s.token[j]; });
   double sum = 0;
@@ -300,11 +292,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(const VerifyArgs a) {
   sum = wave_sum(sum);
   VerifyState& state = a.state[b];
   if (lane == 0) state.sums[mine] = sum;
-  if (piece == 0) {
-    if (tid == 0) state.cur = cur, state.k = k;
-    if (draft)
-      for (int i = tid; i < k; i += kThreads) state.left[i] = s.left[i];
-  }
+  if (piece == 0 && tid == 0) state.cur = cur, state.k = k, state.S = S;
 }
 
 // The token after the accepted rows: the part, and in it the element, at which the partial sums of r pass u0 times
@@ -317,12 +305,11 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(const VerifyArgs 
   // (loaded together; of an empty run they are anything)
   const int begin = run_offset(a.runs, b), n = min(run_offset(a.runs, b + 1) - begin, a.max_new);
   const int cur = state.cur, k = state.k;
+  const double S = state.S;
   double part_sum = tid < n_parts ? state.sums[tid] : 0.0;
   if (n <= 0) return;
   const double u0 = a.uniform[begin];
-  if (a.draft)
-    for (int i = tid; i < k; i += kThreads) s.left[i] = state.left[i];   // (the scan has barriers)
-  const Row row(a, begin, cur, k, s.left, s.dropped);
+  const Row row(a, begin, cur, k, S, s.dropped);
   double incl, excl;
   double total = block_scan(part_sum, s.wave, &incl, &excl);
   const bool use_p = !(total > 0);
