@@ -69,9 +69,14 @@ int delta_tree_workspace_bytes(const delta_shape_t* shape, int32_t n_rows, int32
  *               from the run's length on are ignored.  A row sees itself only if its own bit is set.
  *   mask_words: >= 1 and at least max_new / 32, rounded up
  *   q, out, max_new, ws, and what is undefined with a run longer than max_new: as in delta_extend_attn, so
- *   also infinite and NaN keys and values (a row gets them of the tokens that it sees, and no others),
- *   max_seq_len, which decides the speed of calls of few rows, and determinism.  Calls of more than 65535 tiles
- *   (as counted there) give DELTA_ERR_UNSUPPORTED.
+ *   also infinite and NaN keys and values (a row gets them of the tokens that it sees, and no others) and
+ *   determinism.  Calls of more than 65535 tiles (as counted there) give DELTA_ERR_UNSUPPORTED.
+ * Up to 256 sequences are shared out over the GPU by their lengths; of more, a workgroup walks a sequence alone,
+ * and the longest decides (8 rows each, 32/8 heads, one of 65536 tokens among 300s: 160 us for 256 sequences, 708
+ * for 257; where all are 500 to 8192 tokens long 805 and 791).  max_seq_len decides how a call is cut: far above the
+ * lengths it takes up to 1.7 times as long (16 sequences of 300 to 700 tokens, 16 rows, 32/8 heads: 17 us with 700, 29
+ * with 1400 and more; one of 2048, 64 rows: 21 and 25; one of 8192, 16 rows: 21 and 23), and calls that fill the GPU
+ * the same time.
  * bf16 queries, fp32 scores, softmax and sums, one bf16 rounding of the result.  Where they meet the values
  * (their sum is not rounded) the probabilities have 16 bits: over e4m3 caches those of fp16 (at most 2^-11 of
  * each); over bf16 caches two bf16 terms (2^-16) where runs have up to 32 rows a KV head (max_new * G, G query

@@ -23,7 +23,8 @@
 //
 // LDS layouts: K rows with their 16-byte pieces permuted by the row (16 lanes reading one piece of
 // 16 rows touch all banks), V rows with their 64-byte pieces permuted by the row (the four rows of
-// a transposing read do).  The counters show no bank conflict.
+// a transposing read do): reads have no bank conflicts.  Storing blocks of e4m3 caches as bf16 or fp16 has: lanes store
+// two 16-byte pieces of a row one after the other, 7.8e6 of the 3.05e7 LDS cycles of 12 trees over 10K-32K tokens.
 //
 // Precision.  Scores, maximum, sum and outputs are fp32.  The matrix cores take the inputs of the P V product in 16
 // bits, so there a probability is rounded:
@@ -31,8 +32,8 @@
 //     tree_attn_kernel.hip for the price of a second term);
 //   * trees in tiles of 32 rows of bf16 caches: to two bf16 terms, 2^-16 of each (kTwoTerms), which costs little
 //     where the cache's bytes or a chain of loads decide;
-//   * trees over e4m3 caches: to fp16, 2^-11 of each (kHalf).  fp16 holds every e4m3 value, and the conversions and
-//     products of both types take the same time.
+//   * trees over e4m3 caches: to fp16, 2^-11 of each (kHalf).  fp16 holds every e4m3 value, and its conversions
+//     and products are as fast as bf16's.
 #pragma once
 
 #include <algorithm>

@@ -16,8 +16,8 @@
 // Bound: the copy rate for prompts (86423 rows of 40/8 heads into an e4m3 cache, 2.3 GB in 431 us, 5.3
 // TB/s, where a plain copy runs at 5.0), launch and the chain of lookups (offset, length, page) for a
 // few rows (one row 3.6 us in a graph).
-// With a norm the same: 9351 rows of 32/8 heads, 230 MB on changing inputs in 47.7 us, 4.8 TB/s; a tree of
-// 16 rows of 28/4 heads 4.5 us.
+// With a norm the same: 9351 rows of 32/8 heads, 230 MB on changing inputs, calls one after another 47.8 us, 4.8
+// TB/s; a tree of 16 rows of 28/4 heads 4.8 us.
 #include "debug_check.h"
 #include "runs.h"
 

@@ -21,20 +21,22 @@
 // and 132, 32 short ones 10.1 and 9.9, one tree of 16 behind 8192 tokens, 28/4 heads, 19.8 and 20.5, one of 64 behind 2048
 // 20.3 and 21.5.  Tiles of 256 rows would pay for them (16 sequences of 4K-16K, 32/8 heads, 16 nodes 147 and 169, 32
 // nodes 178 and 209, 64 of each 238 and 300) and keep the one: 1.69e-3 rms off float64 instead of the output's own
-// rounding's 1.66e-3.  e4m3 caches: two bf16 terms took 284 where one takes 168 (12 trees of 8 to 24 nodes, 40/8 heads),
+// rounding's 1.66e-3.  e4m3 caches: two bf16 terms took 284 where one takes 167 (12 trees of 8 to 24 nodes, 40/8 heads),
 // fp16 169.
 //
-// Bound.  256 rows: issue, at the lower clock that loads and products together leave: 16 trees of 64 nodes behind 4K-16K
-// tokens, 32/8 heads, 217 us at 2.03 GHz (834 TFLOP/s, VALU 50 % and MFMA 40 % of the SIMDs' cycles) and 12 us for the
-// join, which reads 48 MB of parts.  In an earlier state, 232 us together, taking the loads out left 164, taking the
-// products out 154.
-// 33 to 128 rows of bf16: HBM, 16 of 4K-16K with 16 nodes 146 us together (4.8 TB/s); of e4m3: phases that follow one
-// another between the barriers (loads, conversion, products, softmax; VALU 33 %, LDS 30 %, MFMA 24 %), 12 of 10K-32K with
-// 8 to 24 nodes, 40/8 heads, 156 us and 6.5 for the join.  Measured slower or equal there: tiles of 128 rows by four waves,
-// two workgroups a CU (bf16 -9 % to +3 %, e4m3 +18 % to +26 %), e4m3 blocks through a ring of two (+1 % to +4 %).
-// Few rows: 16 of 4K-16K with 8 nodes 131 us together (5.4 TB/s); with a row of units per head instead of groups that
-// walk the same pages at the same time 138.  One tree of 16 behind 8192 tokens, 28/4 heads: 14.6 and 3.2 for the join;
-// behind 64 tokens, in one launch, 7.1 in a graph: the chain offsets -> queries, masks and pages -> blocks.
+// Bound (medians of 200 dispatches).  256 rows: issue, at the lower clock that loads and products together leave: 16
+// trees of 64 nodes behind 4K-16K tokens, 32/8 heads, 237 us (763 TFLOP/s; the least 217, 835) at 2.01 GHz, VALU 50 %
+// and MFMA 39 % of the SIMDs' cycles, and 12 for the join, which reads 48 MB of parts.  In an earlier state, 232 us
+// together, taking the loads out left 164, taking the products out 154.
+// 33 to 128 rows of bf16: HBM, 16 of 4K-16K with 16 nodes 128 us and 5 (in a graph 147 together, 4.7 TB/s); of e4m3:
+// phases that follow one another between the barriers (loads, conversion, products, softmax; VALU 38 %, LDS 32 %, MFMA
+// 26 %), 12 of 10K-32K with 8 to 24 nodes, 40/8 heads, 169 us and 7.  Measured slower or equal there: tiles of 128 rows by
+// four waves, two workgroups a CU (bf16 -9 % to +3 %, e4m3 +18 % to +26 %), e4m3 blocks through a ring of two (+1 % to
+// +4 %).
+// Few rows: 16 of 4K-16K with 8 nodes 117 us and 5 (in a graph 132 together, 5.4 TB/s; e4m3 76 and 5); with a row of
+// units per head instead of groups that walk the same pages at the same time 5 % more.  One tree of 16 behind 8192
+// tokens, 28/4 heads: 17.7 and 4.0 for the join; behind 64 tokens, in one launch, 7.4 in a graph: the chain offsets ->
+// queries, masks and pages -> blocks.
 #include "attend_runs.h"
 #include "drafts.h"
 

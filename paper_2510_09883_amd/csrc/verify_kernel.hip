@@ -15,9 +15,10 @@
 // residual.  A second launch finds the part, and in it the token, at which the partial sums pass u0 R.  Every sum
 // has a fixed order, so equal calls give equal tokens.
 //
-// Bound: latencies, of launches and of the chains offsets -> parents -> values -> row and sums -> row (one tree of 16
-// chosen drafts, 151936 tokens: 5.3 us and 3.7); then the reads of the rows (64 chains of drawn drafts, 78 MB: 17 us, 4.6
-// TB/s, and 4.5).  Measured for the chains, both launches in a graph: finding the token by LDS atomics of all threads on
+// Bound (medians of 200 dispatches): latencies, of launches and of the chains offsets -> parents -> values -> row and sums -> row (one tree of 16
+// chosen drafts, 151936 tokens: 5.6 us and 4.0); then the reads of the rows (64 chains of drawn drafts, of which 41 end in a
+// rejection and read the drafts' row too, 64 MB: 16.4 us, 3.9 TB/s, and 4.6).  A sum of R over 151936 tokens takes 13 us (16
+// trees of 8 rows, up to three drawn siblings: 33 and 4.8).  Measured for the chains, both launches in a graph: finding the token by LDS atomics of all threads on
 // one word 38 us, by ballots 31; with parts that are whole rounds of 16 bytes a lane, where nearly half of a part was
 // read 4 bytes a lane before, 25.  That the last of a sequence's workgroups to arrive at a counter picks the token was
 // no faster than a second launch (38 us for both), and 208 with release and acquire at the counter.
